@@ -160,7 +160,7 @@ def _prepare_list(c, seed):
     m = g.float() * 0.3
     v = g.float().square() * (0.5 + _rand((size,), seed, 4)) * 1e-2
     if c["bits"] == 8:
-        m, em = _encode_m(m)
+        m, em = _encode_m(m, seed & 0x7FFFFFFF)
         v, ev = _encode_v(v, seed & 0x7FFFFFFF)
         s["state"] = {"m": m, "em": em, "v": v, "ev": ev}
     else:
@@ -194,8 +194,9 @@ def prepare(case, seed):
 
 # --------------------------------------------------- moments held in 8 bits
 def _exponents(x):
-    """per block, the exponent of its largest magnitude (-127 for none)"""
-    return (x.view(-1, BLOCK).abs().amax(1).view(torch.int32) >> 23) - 127
+    """per block, the exponent of the power of two that its largest magnitude
+    lies under once it is rounded up to 3 mantissa bits (-127 for none)"""
+    return ((x.view(-1, BLOCK).abs().amax(1).view(torch.int32) + 0xFFFFF) >> 23) - 127
 
 
 def _scaled(x, e, bias):
@@ -203,21 +204,22 @@ def _scaled(x, e, bias):
     return (x.view(-1, BLOCK).double() * torch.exp2((-bias - e).double())[:, None]).float().view(-1)
 
 
-def _encode_m(m):
-    """sign, 4 exponent bits, 3 mantissa bits, nearest, ties to even"""
+def _encode_m(m, seed):
+    """sign, 4 exponent bits, 3 mantissa bits, up or down at random"""
     e = _exponents(m)
     bits = _scaled(m.abs(), e, 112).view(torch.int32)
-    u = ((bits + 0x7FFFF + ((bits >> 20) & 1)) >> 20).clamp(max=127)
+    u = ((bits + _noise(m.numel(), seed, swap=True)) >> 20).clamp(max=127)
     return (u | torch.where(m.view(torch.int32) < 0, 128, 0)).to(torch.uint8), e.to(torch.int8)
 
 
-def _noise(size, seed):
-    """20 random bits per position: a hash of the position's pair and the seed, 16 bits of it and a half"""
+def _noise(size, seed, swap=False):
+    """20 random bits per position: a hash of the position's pair and the seed, 16 bits of it (swap: the other
+    position's) and a half"""
     j = torch.arange((size + 1) // 2, device=DEV, dtype=torch.int64)
     h = ((j ^ seed) * 0x9E3779B9) & 0xFFFFFFFF
     h = ((h ^ (h >> 15)) * 0xB7E15163) & 0xFFFFFFFF
     h = h ^ (h >> 16)
-    h = torch.stack([h & 0xFFFF, h >> 16], 1).view(-1)[:size]
+    h = torch.stack([h >> 16, h & 0xFFFF] if swap else [h & 0xFFFF, h >> 16], 1).view(-1)[:size]
     return ((h << 4) | 8).to(torch.int32)
 
 
@@ -275,7 +277,7 @@ def _plain_adamw(s):
     s["p"].copy_(p)
     if eight:
         s["seed"] = (s["seed"] + 1) & 0x7FFFFFFF
-        st["m"], st["em"] = _encode_m(m)
+        st["m"], st["em"] = _encode_m(m, s["seed"])
         st["v"], st["ev"] = _encode_v(v, s["seed"])
         m, v = _decode(st["m"], st["em"], 7, 112), _decode(st["v"], st["ev"], 8, 96)
     else:
