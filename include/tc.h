@@ -315,6 +315,81 @@ tc_status tc_aqsgd_reconstruct(const tc_codec* c, const tc_payload* in, void* m_
                                uint64_t n_samples, const int64_t* ids, uint32_t n_ids, void* a_hat,
                                void* stream);
 
+/* ------------------------------------------- gradients and parameters
+ *
+ * What a stage does with its gradients once the backward pass is over.  A call
+ * takes a list of tensors (a host array, read during the call); tensors may
+ * lie at any address that is a multiple of their element size. */
+
+/* One tensor of a list.
+ *   p    parameters [n] (tc_adamw_step: in-out; tc_grad_norm: unused)
+ *   g    gradients [n]
+ *   w32  NULL, or the parameters in binary32 [n], in-out: the step is taken on
+ *        them and p receives their rounding
+ *   n    elements, < 2^40; 0: the tensor is skipped
+ *   pos  first position of its moments, a multiple of 256; the tensor owns
+ *        the positions pos .. pos + 256 * ceil(n / 256) - 1 */
+typedef struct {
+  void* p;
+  const void* g;
+  float* w32;
+  uint64_t n;
+  uint64_t pos;
+} tc_tensor;
+
+/* Workspace bytes of tc_grad_norm for a list of n_list tensors (the rules of
+ * the other workspaces hold). */
+uint64_t tc_grad_norm_workspace_bytes(uint64_t n_list);
+
+/* out[0] = norm = sqrt(sum g^2) over every element of the list, summed in
+ * binary64 and rounded once; out[1] = min(1, max_norm / (norm + 1e-6)), the
+ * factor that clips the gradients.  out: 2 binary32 values on the device.
+ * g_dt: dtype of every g.  The result does not depend on the order in which
+ * workgroups run.  max_norm must be positive. */
+tc_status tc_grad_norm(const tc_tensor* list, uint64_t n_list, int g_dt, float max_norm, float* out, void* ws,
+                       size_t ws_bytes, void* stream);
+
+/* AdamW's settings and moments.
+ *   lr, beta1, beta2, eps, weight_decay   0 <= beta < 1, eps >= 0
+ *   t      this step's number, from 1 on (bias correction)
+ *   bits   32: m and v are binary32 [positions]
+ *          8: m and v are codes (a byte per position) and em, ev the exponents
+ *          (a byte per 256 positions).  With E the exponent of a block's
+ *          largest magnitude rounded up to 3 mantissa bits (-127 for a block
+ *          of zeros), a code of m with magnitude bits u (7) stands for
+ *          +-binary32(u << 20) * 2^(112 + E), of v (8 bits)
+ *          binary32(u << 20) * 2^(96 + E), where binary32(.) reads a bit
+ *          pattern.  Both are rounded up or down with the distances as
+ *          chances, and v not to 0 unless it is 0.  Codes of 0 are the
+ *          moments before the first step, whatever the exponents
+ *   seed   8 bits: the random bits of a step are a hash of the position and
+ *          the seed; take another seed for every step */
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay;
+  uint64_t t;
+  uint32_t bits;
+  uint32_t seed;
+  void* m;
+  void* v;
+  int8_t* em;
+  int8_t* ev;
+} tc_adamw;
+
+/* One AdamW step over the list, in binary32 arithmetic:
+ *   g' = factor g;  m <- beta1 m + (1 - beta1) g';  v <- beta2 v + (1 - beta2) g'^2
+ *   p <- p (1 - lr weight_decay) - (m / (sqrt(v / (1 - beta2^t)) + eps)) lr / (1 - beta1^t)
+ * p_dt, g_dt: dtypes of every p and g.  clip: NULL (factor 1), or the two
+ * values tc_grad_norm wrote; where the norm is not finite, nothing is changed.
+ * (Without it gradients must be finite, and with 8 bits g'^2 too.)  The
+ * tensors' arrays and positions must not overlap. */
+tc_status tc_adamw_step(const tc_adamw* a, const tc_tensor* list, uint64_t n_list, int p_dt, int g_dt,
+                        const float* clip, void* stream);
+
+/* The binary32 values that 8-bit moments stand for: m_out, v_out [n] from the
+ * codes and exponents of n positions (a multiple of 256). */
+tc_status tc_adamw_moments(const uint8_t* m, const int8_t* em, const uint8_t* v, const int8_t* ev, uint64_t n,
+                           float* m_out, float* v_out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -703,5 +704,100 @@ TC_API tc_status tc_aqsgd_reconstruct(const tc_codec* c, const tc_payload* in, v
   a.k = c->k;
   hipError_t he = tc::launch_aqsgd_recv(dt, a, (hipStream_t)stream);
   if (he != hipSuccess) return hip_fail(he, "aqsgd reconstruct launch");
+  return TC_OK;
+}
+
+// ------------------------------------------- gradients and parameters
+static_assert(sizeof(tc_tensor) == sizeof(tc::ListEntry), "one layout");
+
+namespace {
+
+// Of a list's tensors that have elements: sizes, and the pointers and
+// positions that the call uses.
+tc_status check_list(const tc_tensor* list, uint64_t n_list, int g_dt, int p_dt, bool step) {
+  if (n_list > 0 && !list) return fail(TC_ERR_NULL, "list is NULL");
+  if (n_list > (1ull << 24)) return fail(TC_ERR_ARG, "%llu tensors", (unsigned long long)n_list);
+  for (uint64_t k = 0; k < n_list; ++k) {
+    const tc_tensor& t = list[k];
+    const unsigned long long i = k;
+    if (t.n == 0) continue;
+    if (t.n >= (1ull << 40)) return fail(TC_ERR_ARG, "tensor %llu: %llu elements", i, (unsigned long long)t.n);
+    if (!t.g) return fail(TC_ERR_NULL, "tensor %llu: g is NULL", i);
+    if ((uintptr_t)t.g % tc::dt_size(g_dt)) return fail(TC_ERR_ALIGN, "tensor %llu: g lies inside an element", i);
+    if (!step) continue;
+    if (!t.p) return fail(TC_ERR_NULL, "tensor %llu: p is NULL", i);
+    if ((uintptr_t)t.p % tc::dt_size(p_dt)) return fail(TC_ERR_ALIGN, "tensor %llu: p lies inside an element", i);
+    if ((uintptr_t)t.w32 % 4u) return fail(TC_ERR_ALIGN, "tensor %llu: w32 lies inside an element", i);
+    if (t.pos % 256u || t.pos >= (1ull << 44)) return fail(TC_ERR_ARG, "tensor %llu: pos %llu", i, (unsigned long long)t.pos);
+  }
+  return TC_OK;
+}
+
+}  // namespace
+
+TC_API uint64_t tc_grad_norm_workspace_bytes(uint64_t n_list) { return tc::grad_norm_ws_bytes(n_list); }
+
+TC_API tc_status tc_grad_norm(const tc_tensor* list, uint64_t n_list, int g_dt, float max_norm, float* out, void* ws,
+                              size_t ws_bytes, void* stream) {
+  if (!dt_ok(g_dt)) return fail(TC_ERR_DTYPE, "gradient dtype %d", g_dt);
+  const tc_status s = check_list(list, n_list, g_dt, 0, false);
+  if (s != TC_OK) return s;
+  if (!(max_norm > 0.0f)) return fail(TC_ERR_ARG, "max_norm must be positive");
+  if (!out) return fail(TC_ERR_NULL, "out is NULL");
+  const uint64_t need = tc::grad_norm_ws_bytes(n_list);
+  if (!ws || ws_bytes < need)
+    return fail(TC_ERR_WORKSPACE, "workspace %zu bytes < %llu required", ws ? ws_bytes : (size_t)0, (unsigned long long)need);
+  if (((uintptr_t)ws & 7u) != 0) return fail(TC_ERR_ALIGN, "workspace must be 8-byte aligned");
+  const hipError_t he = tc::launch_grad_norm(g_dt, (const tc::ListEntry*)list, n_list, max_norm, out, ws, (hipStream_t)stream);
+  if (he != hipSuccess) return hip_fail(he, "gradient norm launch");
+  return TC_OK;
+}
+
+TC_API tc_status tc_adamw_step(const tc_adamw* a, const tc_tensor* list, uint64_t n_list, int p_dt, int g_dt,
+                               const float* clip, void* stream) {
+  if (!a) return fail(TC_ERR_NULL, "settings are NULL");
+  if (!dt_ok(p_dt) || !dt_ok(g_dt)) return fail(TC_ERR_DTYPE, "dtypes %d, %d", p_dt, g_dt);
+  if (a->bits != 8 && a->bits != 32) return fail(TC_ERR_ARG, "bits %u, not 8 or 32", a->bits);
+  if (!(a->beta1 >= 0.0 && a->beta1 < 1.0 && a->beta2 >= 0.0 && a->beta2 < 1.0))
+    return fail(TC_ERR_ARG, "beta1 %g, beta2 %g not in [0, 1)", a->beta1, a->beta2);
+  if (!(a->eps >= 0.0) || !std::isfinite(a->eps) || !std::isfinite(a->lr) || !std::isfinite(a->weight_decay))
+    return fail(TC_ERR_ARG, "lr %g, eps %g, weight_decay %g", a->lr, a->eps, a->weight_decay);
+  if (a->t == 0) return fail(TC_ERR_ARG, "steps are counted from 1");
+  const tc_status s = check_list(list, n_list, g_dt, p_dt, true);
+  if (s != TC_OK) return s;
+  bool any = false;
+  for (uint64_t k = 0; k < n_list && !any; ++k) any = list[k].n > 0;
+  if (!any) return TC_OK;
+  if (!a->m || !a->v || (a->bits == 8 && (!a->em || !a->ev))) return fail(TC_ERR_NULL, "moments are NULL");
+  if (a->bits == 32 && (((uintptr_t)a->m | (uintptr_t)a->v) & 3u))
+    return fail(TC_ERR_ALIGN, "binary32 moments must be 4-byte aligned");
+  tc::AdamwArgs k{};
+  k.m = a->m;
+  k.v = a->v;
+  k.em = a->em;
+  k.ev = a->ev;
+  k.clip = clip;
+  k.b1 = (float)a->beta1;
+  k.a1 = (float)(1.0 - a->beta1);
+  k.b2 = (float)a->beta2;
+  k.a2 = (float)(1.0 - a->beta2);
+  k.decay = (float)(1.0 - a->lr * a->weight_decay);
+  k.r2 = (float)(1.0 / (1.0 - std::pow(a->beta2, (double)a->t)));
+  k.eps = (float)a->eps;
+  k.rate = (float)(a->lr / (1.0 - std::pow(a->beta1, (double)a->t)));
+  k.seed = a->seed;
+  const hipError_t he = tc::launch_adamw(p_dt, g_dt, (int)a->bits, k, (const tc::ListEntry*)list, n_list, (hipStream_t)stream);
+  if (he != hipSuccess) return hip_fail(he, "adamw launch");
+  return TC_OK;
+}
+
+TC_API tc_status tc_adamw_moments(const uint8_t* m, const int8_t* em, const uint8_t* v, const int8_t* ev, uint64_t n,
+                                  float* m_out, float* v_out, void* stream) {
+  if (n % 256u || n >= (1ull << 44)) return fail(TC_ERR_ARG, "%llu positions", (unsigned long long)n);
+  if (n == 0) return TC_OK;
+  if (!m || !em || !v || !ev || !m_out || !v_out) return fail(TC_ERR_NULL, "a moment pointer is NULL");
+  if (((uintptr_t)m_out | (uintptr_t)v_out) & 3u) return fail(TC_ERR_ALIGN, "outputs must be 4-byte aligned");
+  const hipError_t he = tc::launch_moments({m, v, em, ev, m_out, v_out, n}, (hipStream_t)stream);
+  if (he != hipSuccess) return hip_fail(he, "moments launch");
   return TC_OK;
 }

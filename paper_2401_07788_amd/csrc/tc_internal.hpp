@@ -158,6 +158,60 @@ uint64_t global_ws_words(uint64_t L);
 void global_ws_carve(uint32_t* ws, uint64_t L, GlobalArgs& a);
 hipError_t launch_global(int dt, bool ef, uint32_t qbits, const GlobalArgs& a, hipStream_t st);
 
+// ------------------------------------------- lists of tensors (k_optim.hip)
+struct ListEntry {
+  void* p;               // parameters
+  const void* g;         // gradients
+  float* w32;            // binary32 parameters that p is the rounding of, or nullptr
+  uint64_t n;            // elements
+  uint64_t pos;          // first position in the moments
+};
+// as many tensors as keep a launch's arguments under 4 KB
+constexpr uint32_t ADAMW_LIST = 88, NORM_LIST = 192;
+struct AdamwArgs {
+  ListEntry t[ADAMW_LIST];
+  uint32_t first[ADAMW_LIST];   // each tensor's first chunk
+  void* m;               // binary32 values or codes
+  void* v;
+  int8_t* em;            // 8 bits: exponents, one per 256 positions
+  int8_t* ev;
+  const float* clip;     // (norm, factor) or nullptr
+  uint32_t n, chunk;     // tensors; elements of a workgroup
+  float b1, a1, b2, a2;  // beta and 1 - beta
+  float decay;           // 1 - lr wd
+  float r2, eps, rate;   // 1 / (1 - beta2^t), eps, lr / (1 - beta1^t)
+  uint32_t seed;
+};
+static_assert(sizeof(AdamwArgs) <= 4096, "kernel arguments");
+hipError_t launch_adamw(int p_dt, int g_dt, int bits, AdamwArgs& a, const ListEntry* list, uint64_t n_list, hipStream_t st);
+
+struct MomentsArgs {
+  const uint8_t* m;
+  const uint8_t* v;
+  const int8_t* em;
+  const int8_t* ev;
+  float* m_out;
+  float* v_out;
+  uint64_t n;            // positions, a multiple of 256
+};
+hipError_t launch_moments(const MomentsArgs& a, hipStream_t st);
+
+constexpr uint32_t NORM_GRID = 2048;   // workgroups of a launch, each with one partial sum
+struct NormArgs {
+  struct { const void* g; uint64_t n; } t[NORM_LIST];
+  uint32_t first[NORM_LIST];
+  double* part;          // partial sums of every launch
+  uint32_t* count;       // workgroups of the last launch that are done
+  float* out;            // (norm, factor)
+  uint32_t n, chunk, chunks;
+  uint32_t slot, slots;  // this launch's first partial sum; all of them (0: not the last launch)
+  float max_norm;
+};
+static_assert(sizeof(NormArgs) <= 4096, "kernel arguments");
+uint64_t grad_norm_ws_bytes(uint64_t n_list);
+hipError_t launch_grad_norm(int g_dt, const ListEntry* list, uint64_t n_list, float max_norm, float* out, void* ws,
+                            hipStream_t st);
+
 // ------------------------------------ preconditions (debug library only)
 // Bits the check kernels of k_check.hip report; each call synchronizes the
 // stream and returns the bits found (and clears them).

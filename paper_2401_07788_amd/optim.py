@@ -1,0 +1,161 @@
+"""What a pipeline stage does with its gradients once the backward pass is
+over: their global norm (with the factor that clips them, left on the device)
+and an AdamW step over all of its tensors at once, with moments in binary32 or
+in 8 bits.  Argument marshalling only: the arithmetic is in the HIP kernels of
+libtc.so (include/tc.h), and there is no fallback."""
+from __future__ import annotations
+
+import ctypes as C
+import math
+
+import torch
+
+from . import tc
+
+BLOCK = 256     # positions of 8-bit moments that share an exponent
+
+
+def _check_tensors(ts, what: str):
+    """one dtype, one device, contiguous"""
+    if not ts:
+        raise ValueError(f"{what}: an empty list")
+    dtype, device = ts[0].dtype, ts[0].device
+    if dtype not in tc._DT:
+        raise TypeError(f"unsupported dtype {dtype}")
+    for t in ts:
+        if t.dtype != dtype:
+            raise TypeError(f"{what}: {t.dtype} among {dtype}")
+        if t.device != device:
+            raise ValueError(f"{what}: tensors on {t.device} and {device}")
+        if not t.is_contiguous():
+            raise ValueError("libtc needs contiguous tensors")
+    return dtype, device
+
+
+class TensorList:
+    """tensors of one dtype on one device, as the library takes them: a table
+    of addresses and sizes made once.  It keeps the tensors."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self.dtype, self.device = _check_tensors(self.tensors, "tensors")
+        self.table = (tc.Tensor * len(self.tensors))()
+        for row, t in zip(self.table, self.tensors):
+            row.g, row.n = t.data_ptr(), t.numel()
+        self.ws_bytes = int(tc.lib().tc_grad_norm_workspace_bytes(len(self.tensors)))
+
+
+def grad_norm(grads, max_norm: float, out: torch.Tensor = None, ws: torch.Tensor = None) -> torch.Tensor:
+    """float32 [2]: the norm over all tensors of `grads` (a TensorList or
+    tensors), and min(1, max_norm / (norm + 1e-6)), the factor that clips them"""
+    lst = grads if isinstance(grads, TensorList) else TensorList(grads)
+    tc._need_gpu(lst.tensors[0], out)
+    if out is None:
+        out = torch.empty(2, dtype=torch.float32, device=lst.device)
+    elif out.dtype != torch.float32 or out.numel() != 2 or out.device != lst.device:
+        raise ValueError(f"out must be float32 [2] on {lst.device}")
+    st = tc._stream(lst.device)
+    if ws is None:
+        ws = tc._ws_cache.get((lst.device.index, st))
+        if ws is None or ws.numel() < lst.ws_bytes:
+            ws = tc._workspace_of(lst.ws_bytes, lst.device)
+    tc._check(tc.lib().tc_grad_norm(lst.table, len(lst.table), tc._DT[lst.dtype], max_norm, out.data_ptr(),
+                                    ws.data_ptr(), ws.numel() * ws.element_size(), st), "tc_grad_norm")
+    return out
+
+
+class AdamW:
+    """AdamW over a stage's parameters (tensors of one dtype on one device,
+    updated in place).
+
+    state_bits  32: binary32 moments; 8: codes with an exponent per 256 positions
+    master      keep the parameters in binary32 beside 16-bit ones, which
+                receive their rounding
+    state       moments to go on from (as `state` holds them), else zeros
+    t, seed     steps taken so far, and the seed of 8-bit rounding (the
+                step's number is added to it)
+
+    Positions: each tensor's moments start at a multiple of 256 in the flat
+    arrays `state["m"]` and `state["v"]`; places[k] is tensor k's first."""
+
+    def __init__(self, params, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
+                 state_bits: int = 32, master: bool = False, state: dict = None, t: int = 0, seed: int = 0):
+        self.params = list(params)
+        self.dtype, self.device = _check_tensors(self.params, "params")
+        if state_bits not in (8, 32):
+            raise ValueError(f"state_bits {state_bits}, not 8 or 32")
+        self.lr, self.betas, self.eps, self.weight_decay = lr, betas, eps, weight_decay
+        self.bits, self.t, self.seed = state_bits, t, seed
+        self.places, size = [], 0
+        for p in self.params:
+            self.places.append(size)
+            size += -(-p.numel() // BLOCK) * BLOCK
+        self.size = size
+        self.state = state if state is not None else self._zeros()
+        self._check_state()
+        self.w32 = [p.detach().float() for p in self.params] if master and self.dtype != torch.float32 else None
+        self.table = (tc.Tensor * len(self.params))()
+        for k, (row, p) in enumerate(zip(self.table, self.params)):
+            row.p, row.n, row.pos = p.data_ptr(), p.numel(), self.places[k]
+            row.w32 = self.w32[k].data_ptr() if self.w32 else None
+
+    def _spec(self):
+        if self.bits == 32:
+            return {"m": (self.size, torch.float32), "v": (self.size, torch.float32)}
+        blocks = self.size // BLOCK
+        return {"m": (self.size, torch.uint8), "v": (self.size, torch.uint8),
+                "em": (blocks, torch.int8), "ev": (blocks, torch.int8)}
+
+    def _zeros(self):
+        return {k: torch.zeros(n, dtype=dt, device=self.device) for k, (n, dt) in self._spec().items()}
+
+    def _check_state(self):
+        for k, (n, dt) in self._spec().items():
+            s = self.state.get(k)
+            if s is None or s.dtype != dt or s.dim() != 1 or s.numel() != n or s.device != self.device or \
+                    not s.is_contiguous():
+                raise ValueError(f"state[{k!r}] must be {dt} [{n}] on {self.device}")
+
+    def step(self, grads=None, clip: torch.Tensor = None):
+        """one step.  grads: a tensor per parameter (of one dtype), else their
+        .grad; clip: what grad_norm returned, else the gradients as they are.
+        Where the norm is not finite nothing is changed but the step count."""
+        if grads is None:
+            grads = [p.grad for p in self.params]
+        if len(grads) != len(self.params):
+            raise ValueError(f"{len(grads)} gradients for {len(self.params)} parameters")
+        gdt, dev = grads[0].dtype, self.device
+        for row, g in zip(self.table, grads):
+            if g.dtype != gdt or g.device != dev:
+                raise TypeError(f"gradients must be of one dtype on {dev}")
+            if g.numel() != row.n or not g.is_contiguous():
+                raise ValueError("a gradient does not fit its parameter, or is not contiguous")
+            row.g = g.data_ptr()
+        if gdt not in tc._DT:
+            raise TypeError(f"unsupported dtype {gdt}")
+        if clip is not None and (clip.dtype != torch.float32 or clip.numel() != 2 or clip.device != dev or
+                                 not clip.is_contiguous()):
+            raise ValueError(f"clip must be float32 [2] on {dev}")
+        tc._need_gpu(self.params[0])
+        st = self.state
+        t = self.t + 1
+        a = tc.AdamwSettings(self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay, t, self.bits,
+                             (self.seed + 1) & 0x7FFFFFFF, st["m"].data_ptr(), st["v"].data_ptr(),
+                             tc._ptr(st.get("em")), tc._ptr(st.get("ev")))
+        tc._check(tc.lib().tc_adamw_step(C.byref(a), self.table, len(self.table), tc._DT[self.dtype], tc._DT[gdt],
+                                         tc._ptr(clip), tc._stream(dev)), "tc_adamw_step")
+        self.t, self.seed = t, (self.seed + 1) & 0x7FFFFFFF
+
+    def moments(self):
+        """(m, v) as float32 [positions]: the state itself, or the values that
+        its codes stand for"""
+        st = self.state
+        if self.bits == 32:
+            return st["m"], st["v"]
+        m = torch.empty(self.size, dtype=torch.float32, device=self.device)
+        v = torch.empty_like(m)
+        tc._need_gpu(m)
+        tc._check(tc.lib().tc_adamw_moments(st["m"].data_ptr(), st["em"].data_ptr(), st["v"].data_ptr(),
+                                            st["ev"].data_ptr(), self.size, m.data_ptr(), v.data_ptr(),
+                                            tc._stream(self.device)), "tc_adamw_moments")
+        return m, v

@@ -42,6 +42,17 @@ class Payload(C.Structure):
                 ("blk", C.c_void_p)]
 
 
+class Tensor(C.Structure):
+    """one tensor of a list (tc_tensor)"""
+    _fields_ = [("p", C.c_void_p), ("g", C.c_void_p), ("w32", C.c_void_p), ("n", C.c_uint64), ("pos", C.c_uint64)]
+
+
+class AdamwSettings(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("weight_decay", C.c_double), ("t", C.c_uint64), ("bits", C.c_uint32), ("seed", C.c_uint32),
+                ("m", C.c_void_p), ("v", C.c_void_p), ("em", C.c_void_p), ("ev", C.c_void_p)]
+
+
 BLOCK_LEN = 4096   # TC_BLOCK_LEN
 
 
@@ -101,6 +112,13 @@ EXPORTS = {
                                         C.c_void_p, C.c_uint32, C.POINTER(Payload), C.c_void_p]),
     "tc_aqsgd_reconstruct": (C.c_int, [C.POINTER(Codec), C.POINTER(Payload), C.c_void_p, C.c_int, C.c_uint64,
                                        C.c_void_p, C.c_uint32, C.c_void_p, C.c_void_p]),
+    "tc_grad_norm_workspace_bytes": (C.c_uint64, [C.c_uint64]),
+    "tc_grad_norm": (C.c_int, [C.c_void_p, C.c_uint64, C.c_int, C.c_float, C.c_void_p, C.c_void_p, C.c_size_t,
+                               C.c_void_p]),
+    "tc_adamw_step": (C.c_int, [C.POINTER(AdamwSettings), C.c_void_p, C.c_uint64, C.c_int, C.c_int, C.c_void_p,
+                                C.c_void_p]),
+    "tc_adamw_moments": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p,
+                                   C.c_void_p, C.c_void_p]),
     "tc_efmix_counts": (None, [C.c_uint64, C.POINTER(C.c_uint64), C.POINTER(C.c_uint64)]),
 }
 
@@ -264,8 +282,10 @@ def workspace(c: Codec, device=None) -> torch.Tensor | None:
     and stream (every completed call leaves it zero-filled again)"""
     device = torch.device(device or torch.cuda.current_device())
     n = workspace_bytes(c)
-    if n == 0:
-        return None
+    return None if n == 0 else _workspace_of(n, device)
+
+
+def _workspace_of(n: int, device) -> torch.Tensor:
     key = (device.index, torch.cuda.current_stream(device).cuda_stream)
     ws = _ws_cache.get(key)
     if ws is None or ws.numel() < n:
