@@ -99,7 +99,7 @@ typedef enum {
 /* kernel-side error bits reported by tc_device_errors() */
 #define TC_KERR_TIMEOUT 1u    /* a cross-workgroup wait gave up; results and workspace invalid */
 #define TC_KERR_BAD_ID 2u     /* an AQ-SGD sample id was outside [0, n_samples); that row was skipped */
-#define TC_KERR_BAD_INDEX 4u  /* a payload index lay outside its segment; the entry was skipped */
+#define TC_KERR_BAD_INDEX 4u  /* a payload index lay outside its segment, or a target outside the vocabulary; it was skipped */
 #define TC_KERR_INTERNAL 8u   /* a selection placed more than k entries (a library fault); extra entries dropped */
 
 /* What one compression operator does to a tensor of n_seg * seg_len elements.
@@ -314,6 +314,54 @@ tc_status tc_aqsgd_step_noalloc(const tc_codec* c, const void* a, int dt, void* 
 tc_status tc_aqsgd_reconstruct(const tc_codec* c, const tc_payload* in, void* m_r, int dt,
                                uint64_t n_samples, const int64_t* ids, uint32_t n_ids, void* a_hat,
                                void* stream);
+
+/* ---------------------------------------------------- the last stage's loss
+ *
+ * What the last stage does with the hidden state that crossed the boundary:
+ * softmax cross entropy of its products with the vocabulary's weights, and the
+ * gradients, of which dx goes back across the boundary. */
+
+/* The sizes of a call.
+ *   n, v, h   tokens (< 2^31), vocabulary (1 .. 2^22), hidden size (1 .. 2^20)
+ *   ldx, ldw  elements from one row of x and of w to the next, >= h
+ *   dt        dtype of x, w, dx and dw
+ *   ignore    target of tokens that do not count: their loss, lse and dx are 0
+ *             and they add nothing to dw, whatever their row of x holds.  A
+ *             target that is neither this nor in [0, v) is taken the same way
+ *             and sets TC_KERR_BAD_INDEX
+ *   chunk     tokens whose softmax entries the workspace holds at once (rounded
+ *             up to a multiple of 64 and to 128 at least), or 0: as many as
+ *             4 GiB hold.  With more than one chunk dw is summed in binary32
+ *             and rounded after the last */
+typedef struct {
+  uint64_t n, v, h, ldx, ldw;
+  int64_t ignore;
+  uint64_t chunk;
+  int32_t dt;
+  uint32_t reserved;   /* must be 0 */
+} tc_xent;
+
+/* Workspace bytes of tc_xent_loss (grad 0) or tc_xent_step (grad 1).  It needs
+ * no particular contents, and 256-byte alignment. */
+tc_status tc_xent_workspace_bytes(const tc_xent* c, int grad, size_t* bytes);
+
+/* loss[i] = lse[i] - z[target[i]] and lse[i] = log sum_v exp z[v] with
+ * z[v] = sum_k x[i][k] w[v][k], products and sums in binary32 (binary32 inputs
+ * are multiplied as pairs of binary16 values: 22 bits of an element down to
+ * 2^-28 of the largest magnitude of its matrix).  loss, lse: [n] binary32;
+ * target: [n] on the device. */
+tc_status tc_xent_loss(const tc_xent* c, const void* x, const void* w, const int64_t* target, float* loss, float* lse,
+                       void* ws, size_t ws_bytes, void* stream);
+
+/* The same, and the gradients of sum_i weight[i] loss[i]:
+ *   d[i][v] = weight[i] (exp(z[v] - lse[i]) - [v == target[i]]),
+ *   dx = d w [n][h],  dw = d^T x [v][h],  rounded to dt after the last sum.
+ * weight: [n] binary32, or NULL (1).  Into the two products d goes with the
+ * significand of dt (binary32: 22 bits); bfloat16 keeps its range, binary16
+ * and binary32 reach down to 2^-28 of the largest in full and to 2^-38 at the
+ * least. */
+tc_status tc_xent_step(const tc_xent* c, const void* x, const void* w, const int64_t* target, const float* weight,
+                       float* loss, float* lse, void* dx, void* dw, void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------- gradients and parameters
  *

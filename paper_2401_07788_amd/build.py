@@ -24,7 +24,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libtc.so")
 LIB_DEBUG = os.path.join(HERE, "libtc_debug.so")
 KERNELS = ["k_topk.hip", "k_quant.hip", "k_scatter.hip", "k_global.hip", "k_scratch.hip",
-           "k_optim.hip"]
+           "k_optim.hip", "k_head.hip"]
 API = "tc_api.cpp"
 CHECKS = "k_check.hip"
 ARCH = "gfx950"

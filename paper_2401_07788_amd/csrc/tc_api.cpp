@@ -404,7 +404,9 @@ TC_API tc_status tc_device_errors(uint32_t* bits, int clear) {
   if ((e = tc::errors_scatter(&d, clear != 0)) != hipSuccess) return hip_fail(e, "error word (scatter)");
   uint32_t g = 0;
   if ((e = tc::errors_global(&g, clear != 0)) != hipSuccess) return hip_fail(e, "error word (global)");
-  *bits = a | b | d | g;
+  uint32_t h = 0;
+  if ((e = tc::errors_head(&h, clear != 0)) != hipSuccess) return hip_fail(e, "error word (head)");
+  *bits = a | b | d | g | h;
   // a wait that gave up leaves the allocation-free entry point's scratch dirty
   if (clear && (*bits & TC_KERR_TIMEOUT) && (e = tc::noalloc_scratch_reset()) != hipSuccess)
     return hip_fail(e, "clearing the scratch");
@@ -420,6 +422,7 @@ TC_API tc_status tc_raise_device_errors(uint32_t bits) {
   if ((e = tc::errors_quant_raise(bits)) != hipSuccess) return hip_fail(e, "error word (quant)");
   if ((e = tc::errors_scatter_raise(bits)) != hipSuccess) return hip_fail(e, "error word (scatter)");
   if ((e = tc::errors_global_raise(bits)) != hipSuccess) return hip_fail(e, "error word (global)");
+  if ((e = tc::errors_head_raise(bits)) != hipSuccess) return hip_fail(e, "error word (head)");
   return TC_OK;
 }
 
@@ -705,6 +708,101 @@ TC_API tc_status tc_aqsgd_reconstruct(const tc_codec* c, const tc_payload* in, v
   hipError_t he = tc::launch_aqsgd_recv(dt, a, (hipStream_t)stream);
   if (he != hipSuccess) return hip_fail(he, "aqsgd reconstruct launch");
   return TC_OK;
+}
+
+// ---------------------------------------------------- the last stage's loss
+namespace {
+
+tc_status check_xent(const tc_xent* c) {
+  if (!c) return fail(TC_ERR_NULL, "sizes are NULL");
+  if (!dt_ok(c->dt)) return fail(TC_ERR_DTYPE, "dtype %d", c->dt);
+  if (c->reserved != 0) return fail(TC_ERR_ARG, "reserved must be 0");
+  if (c->n >= (1ull << 31)) return fail(TC_ERR_ARG, "%llu tokens", (unsigned long long)c->n);
+  if (c->v == 0 || c->v > (1ull << 22)) return fail(TC_ERR_ARG, "vocabulary of %llu", (unsigned long long)c->v);
+  if (c->h == 0 || c->h > (1ull << 20)) return fail(TC_ERR_ARG, "hidden size %llu", (unsigned long long)c->h);
+  if (c->ldx < c->h || c->ldw < c->h || c->ldx > (1ull << 40) || c->ldw > (1ull << 40))
+    return fail(TC_ERR_ARG, "row distances %llu, %llu for rows of %llu", (unsigned long long)c->ldx,
+                (unsigned long long)c->ldw, (unsigned long long)c->h);
+  if (c->chunk > (1ull << 22)) return fail(TC_ERR_ARG, "chunk of %llu tokens", (unsigned long long)c->chunk);
+  return TC_OK;
+}
+
+tc_status xent_common(const tc_xent* c, bool grad, const void* x, const void* w, const int64_t* target,
+                      const float* weight, float* loss, float* lse, void* dx, void* dw, void* ws, size_t ws_bytes,
+                      void* stream) {
+  tc_status s = check_xent(c);
+  if (s != TC_OK) return s;
+  if (c->n > 0 && (!x || !w || !target || !loss || !lse)) return fail(TC_ERR_NULL, "an input or output is NULL");
+  if (grad && ((c->n > 0 && !dx) || !dw || !w)) return fail(TC_ERR_NULL, "a gradient or w is NULL");
+  const uint64_t e = tc::dt_size(c->dt);
+  if (((uintptr_t)x | (uintptr_t)w | (uintptr_t)dx | (uintptr_t)dw) % e)
+    return fail(TC_ERR_ALIGN, "x, w, dx or dw lies inside an element");
+  if (c->n == 0 && !grad) return TC_OK;
+  const uint64_t nx = c->n ? ((c->n - 1) * c->ldx + c->h) * e : 0, nw = ((c->v - 1) * c->ldw + c->h) * e;
+  TC_PRECONDITION(check_disjoint({{x, nx, "x"},
+                                  {w, nw, "w"},
+                                  {target, 8 * c->n, "target"},
+                                  {weight, 4 * c->n, "weight"},
+                                  {loss, 4 * c->n, "loss"},
+                                  {lse, 4 * c->n, "lse"},
+                                  {grad ? dx : nullptr, c->n * c->h * e, "dx"},
+                                  {grad ? dw : nullptr, c->v * c->h * e, "dw"},
+                                  {ws, ws_bytes, "workspace"}}));
+  (void)nx;
+  (void)nw;
+  tc::HeadArgs a{};
+  a.x = x;
+  a.w = w;
+  a.target = target;
+  a.weight = weight;
+  a.loss = loss;
+  a.lse = lse;
+  a.dx = dx;
+  a.dw = dw;
+  a.n = c->n;
+  a.v = c->v;
+  a.h = (uint32_t)c->h;
+  a.ldx = c->ldx;
+  a.ldw = c->ldw;
+  a.ignore = c->ignore;
+  a.chunk = c->chunk;
+  const uint64_t need = tc::head_plan(a, c->dt, grad, (char*)ws);
+  if (!ws || ws_bytes < need)
+    return fail(TC_ERR_WORKSPACE, "workspace %zu bytes < %llu required", ws ? ws_bytes : (size_t)0, (unsigned long long)need);
+  if (((uintptr_t)ws & 255u) != 0) return fail(TC_ERR_ALIGN, "workspace must be 256-byte aligned");
+  const hipError_t he = tc::launch_head(a, c->dt, grad, (hipStream_t)stream);
+  if (he != hipSuccess) return hip_fail(he, "loss launch");
+  return TC_OK;
+}
+
+}  // namespace
+
+TC_API tc_status tc_xent_workspace_bytes(const tc_xent* c, int grad, size_t* bytes) {
+  if (!bytes) return fail(TC_ERR_NULL, "bytes is NULL");
+  const tc_status s = check_xent(c);
+  if (s != TC_OK) return s;
+  tc::HeadArgs a{};
+  a.n = c->n;
+  a.v = c->v;
+  a.h = (uint32_t)c->h;
+  a.ldx = c->ldx;
+  a.ldw = c->ldw;
+  a.chunk = c->chunk;
+  // operands that may turn out to need packing (their addresses decide): as if they did
+  a.x = a.w = (const void*)1;
+  *bytes = (size_t)tc::head_plan(a, c->dt, grad != 0, nullptr);
+  return TC_OK;
+}
+
+TC_API tc_status tc_xent_loss(const tc_xent* c, const void* x, const void* w, const int64_t* target, float* loss,
+                              float* lse, void* ws, size_t ws_bytes, void* stream) {
+  return xent_common(c, false, x, w, target, nullptr, loss, lse, nullptr, nullptr, ws, ws_bytes, stream);
+}
+
+TC_API tc_status tc_xent_step(const tc_xent* c, const void* x, const void* w, const int64_t* target,
+                              const float* weight, float* loss, float* lse, void* dx, void* dw, void* ws,
+                              size_t ws_bytes, void* stream) {
+  return xent_common(c, true, x, w, target, weight, loss, lse, dx, dw, ws, ws_bytes, stream);
 }
 
 // ------------------------------------------- gradients and parameters

@@ -158,6 +158,44 @@ uint64_t global_ws_words(uint64_t L);
 void global_ws_carve(uint32_t* ws, uint64_t L, GlobalArgs& a);
 hipError_t launch_global(int dt, bool ef, uint32_t qbits, const GlobalArgs& a, hipStream_t st);
 
+// ------------------------------------- loss over a vocabulary (k_head.hip)
+struct HeadArgs {
+  // the call
+  const void* x;         // [n][h], rows ldx elements apart
+  const void* w;         // [v][h], rows ldw elements apart
+  const int64_t* target; // [n]
+  const float* weight;   // [n] or nullptr (1)
+  float* loss;           // [n]
+  float* lse;            // [n]
+  void* dx;              // [n][h]
+  void* dw;              // [v][h]
+  uint64_t n, v, ldx, ldw;
+  uint32_t h;
+  int64_t ignore;
+  uint64_t chunk;        // tokens whose softmax is held at once (0: head_plan chooses)
+  // head_plan
+  uint64_t hp, hq, vp;   // h and v rounded up: to 64, 16, 64
+  uint32_t k_logits, k_dx, splits;
+  bool wr_packed, xr_packed, xr_map;
+  uint64_t wr_ld, xr_ld;                                                       // bytes
+  uint64_t wr_plane, xr_plane, wc_plane, xc_plane, pr_plane, pc_plane;         // elements
+  char* info;
+  uint32_t* rows;        // [n] tokens that have a target
+  float* zt;             // [chunk] logit of the target
+  float* row_lse;        // [chunk]
+  float2* stats;         // [pieces][chunk] maximum and sum of a piece of the vocabulary
+  char *wr, *xr;         // operands by rows: w [v][hp], x [chunk][hp] (or the call's own)
+  char *wc, *xc;         // and transposed: [h][vp], [h][chunk]
+  char *pr, *pc;         // softmax minus target: [chunk][vp], [v][chunk]
+  char* pt;              // numerators [chunk][vp] (16-bit types: pr)
+  float* dx_part;        // [splits][chunk][hq]
+  float* dw_sum;         // [v][hq], or nullptr with one chunk
+};
+// bytes that the per-token buffers of a chunk may take unless the caller chooses
+constexpr uint64_t HEAD_CHUNK_BYTES = 4ull << 30;
+uint64_t head_plan(HeadArgs& a, int dt, bool grad, char* base);
+hipError_t launch_head(HeadArgs& a, int dt, bool grad, hipStream_t st);
+
 // ------------------------------------------- lists of tensors (k_optim.hip)
 struct ListEntry {
   void* p;               // parameters
@@ -225,11 +263,13 @@ hipError_t errors_topk(uint32_t* bits, bool clear);
 hipError_t errors_quant(uint32_t* bits, bool clear);
 hipError_t errors_scatter(uint32_t* bits, bool clear);
 hipError_t errors_global(uint32_t* bits, bool clear);
+hipError_t errors_head(uint32_t* bits, bool clear);
 // the same words set from the host (tests of the recovery path)
 hipError_t errors_topk_raise(uint32_t bits);
 hipError_t errors_quant_raise(uint32_t bits);
 hipError_t errors_scatter_raise(uint32_t bits);
 hipError_t errors_global_raise(uint32_t bits);
+hipError_t errors_head_raise(uint32_t bits);
 
 // device properties (cached per device)
 int device_cus();

@@ -42,6 +42,12 @@ class Payload(C.Structure):
                 ("blk", C.c_void_p)]
 
 
+class Xent(C.Structure):
+    """sizes of a loss over a vocabulary (tc_xent)"""
+    _fields_ = [("n", C.c_uint64), ("v", C.c_uint64), ("h", C.c_uint64), ("ldx", C.c_uint64), ("ldw", C.c_uint64),
+                ("ignore", C.c_int64), ("chunk", C.c_uint64), ("dt", C.c_int32), ("reserved", C.c_uint32)]
+
+
 class Tensor(C.Structure):
     """one tensor of a list (tc_tensor)"""
     _fields_ = [("p", C.c_void_p), ("g", C.c_void_p), ("w32", C.c_void_p), ("n", C.c_uint64), ("pos", C.c_uint64)]
@@ -112,6 +118,9 @@ EXPORTS = {
                                         C.c_void_p, C.c_uint32, C.POINTER(Payload), C.c_void_p]),
     "tc_aqsgd_reconstruct": (C.c_int, [C.POINTER(Codec), C.POINTER(Payload), C.c_void_p, C.c_int, C.c_uint64,
                                        C.c_void_p, C.c_uint32, C.c_void_p, C.c_void_p]),
+    "tc_xent_workspace_bytes": (C.c_int, [C.POINTER(Xent), C.c_int, C.POINTER(C.c_size_t)]),
+    "tc_xent_loss": (C.c_int, [C.POINTER(Xent)] + [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]),
+    "tc_xent_step": (C.c_int, [C.POINTER(Xent)] + [C.c_void_p] * 9 + [C.c_size_t, C.c_void_p]),
     "tc_grad_norm_workspace_bytes": (C.c_uint64, [C.c_uint64]),
     "tc_grad_norm": (C.c_int, [C.c_void_p, C.c_uint64, C.c_int, C.c_float, C.c_void_p, C.c_void_p, C.c_size_t,
                                C.c_void_p]),

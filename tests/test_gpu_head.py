@@ -1,0 +1,273 @@
+"""The loss over a vocabulary and its gradients against the definition in 64
+bits, at sizes, strides, masks and values where they can go wrong."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+U = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}       # unit roundoff of the outputs
+# of a softmax entry on its way into the gradient products: the numerator's rounding and the entry's (binary32: 22 bits)
+UD = {"f32": 2.0 ** -20, "bf16": 2.0 ** -11 + 2.0 ** -8, "f16": 2 * 2.0 ** -11}
+IGNORE = -100
+
+
+@pytest.fixture(scope="module")
+def head(tc):
+    from paper_2401_07788_amd import head
+    yield head
+    head.free_workspaces()
+    assert tc.device_errors() == 0
+
+
+def inputs(n, v, h, dt, seed=0, scale=1.0, padx=0, padw=0, shift=0, skip=0.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+
+    def matrix(rows, std, pad):
+        flat = torch.full((rows * (h + pad) + shift + 8,), float("nan"), dtype=DT[dt], device="cuda")
+        m = flat[shift:shift + rows * (h + pad)].view(rows, h + pad)[:, :h]
+        m.copy_(torch.randn(rows, h, generator=g, device="cuda").mul_(std))
+        return m
+
+    x, w = matrix(n, 1.0, padx), matrix(v, 1.5 * scale / math.sqrt(h), padw)
+    t = torch.randint(0, v, (n,), generator=g, device="cuda")
+    t[torch.rand(n, generator=g, device="cuda") < skip] = IGNORE
+    return x, w, t
+
+
+def reference(x, w, t, weight, v):
+    keep = (t >= 0) & (t < v)
+    rows = keep.nonzero()[:, 0]
+    n, h = x.shape
+    xd, wd = x[rows].double().cpu(), w.double().cpu()
+    td, g = t[rows].cpu(), (torch.ones(n) if weight is None else weight.cpu())[rows.cpu()].double()[:, None]
+    z = xd @ wd.t()
+    lse = torch.logsumexp(z, 1) if rows.numel() else torch.zeros(0, dtype=torch.float64)
+    at = torch.arange(rows.numel())
+    out = {k: torch.zeros(n, dtype=torch.float64) for k in ("loss", "lse")}
+    out["loss"][rows.cpu()], out["lse"][rows.cpu()] = lse - z[at, td], lse
+    p = torch.exp(z - lse[:, None])
+    hot = torch.zeros_like(p)
+    hot[at, td] = 1
+    d = g * (p - hot)
+    dx = torch.zeros(n, h, dtype=torch.float64)
+    dx[rows.cpu()] = d @ wd
+    out["dx"], out["dw"] = dx, d.t() @ xd
+    # what the products are made of, for the bounds
+    size = g.abs() * (p + hot)
+    big = torch.zeros(n, h, dtype=torch.float64)
+    big[rows.cpu()] = size @ wd.abs()
+    zs = torch.zeros(n, dtype=torch.float64)
+    if rows.numel():
+        zs[rows.cpu()] = (xd.abs() @ wd.abs().t()).amax(1)
+    return out, {"dx": big, "dw": size.t() @ xd.abs(), "z": zs, "x": xd.abs().sum(0), "top": float(g.abs().max()) if g.numel() else 0.0}
+
+
+def check(r, x, w, t, weight, dt, v):
+    want, size = reference(x, w, t, weight, v)
+    h = x.shape[1]
+    # a logit: products of the inputs are exact (binary32: 22 bits on either side), h sums in binary32 whose
+    # roundings add up as a random walk, four deviations
+    uz = (4 * math.sqrt(h) + 8) * 2.0 ** -24 + (2.0 ** -20 if dt == "f32" else 0)
+    ez = uz * size["z"]
+    # exponentials and sums of positive terms: within 2^-19; the last roundings of lse and of the difference
+    lim = 2 * ez + 2.0 ** -19 + 2.0 ** -22 * (want["lse"].abs() + want["loss"].abs())
+    for k in ("loss", "lse"):
+        got = getattr(r, k).double().cpu()
+        assert torch.isfinite(got).all()
+        assert bool(((got - want[k]).abs() <= lim).all()), (k, float(((got - want[k]).abs() - lim).max()))
+        assert bool((got[(t < 0).cpu()] == 0).all())
+    if not hasattr(r, "dx"):
+        return
+    # an entry is off by its roundings and, relatively, by its logit's and lse's error; the products' sums in binary32
+    rel = UD[dt] + 3 * float(ez.max() if ez.numel() else 0) + 2.0 ** -18 + 64 * 2.0 ** -24
+    low = 2.0 ** -38 if dt != "bf16" else 0.0                 # what binary16 operands reach down to
+    g = torch.ones(x.shape[0]) if weight is None else weight.cpu()
+    lim = rel * size["dx"] + U[dt] * want["dx"].abs() + (2.0 ** -24 if dt == "f16" else 1e-38) + \
+        2 * low * g.double().abs()[:, None] * w.double().cpu().abs().sum(0)
+    err = (r.dx.double().cpu() - want["dx"]).abs()
+    assert bool((err <= lim).all()), ("dx", float((err - lim).max()), float(err.max()))
+    lim = rel * size["dw"] + U[dt] * want["dw"].abs() + (2.0 ** -24 if dt == "f16" else 1e-38) + 2 * low * size["top"] * size["x"]
+    err = (r.dw.double().cpu() - want["dw"]).abs()
+    assert bool((err <= lim).all()), ("dw", float((err - lim).max()), float(err.max()))
+
+
+SIZES = [(1, 1, 1), (1, 50, 64), (3, 2, 5), (17, 129, 33), (64, 255, 64), (65, 256, 32), (100, 257, 96), (128, 1000, 40),
+         (129, 64, 300), (200, 65, 257), (333, 700, 128)]
+
+
+@pytest.mark.parametrize("dt", list(DT))
+@pytest.mark.parametrize("n,v,h", SIZES)
+def test_sizes(head, dt, n, v, h):
+    x, w, t = inputs(n, v, h, dt, seed=n + v)
+    weight = torch.rand(n, device="cuda") + 0.5
+    check(head.linear_xent_step(x, w, t, weight), x, w, t, weight, dt, v)
+    loss, lse = head.linear_xent(x, w, t)
+    assert loss.shape == (n,)
+    check(type("R", (), {"loss": loss, "lse": lse})(), x, w, t, weight, dt, v)
+
+
+@pytest.mark.parametrize("dt", list(DT))
+@pytest.mark.parametrize("padx,padw,shift", [(8, 0, 0), (0, 24, 0), (3, 5, 0), (0, 0, 1), (64, 64, 8)])
+def test_strides_and_addresses(head, dt, padx, padw, shift):
+    n, v, h = 130, 300, 128
+    x, w, t = inputs(n, v, h, dt, 1, padx=padx, padw=padw, shift=shift)
+    check(head.linear_xent_step(x, w, t), x, w, t, None, dt, v)
+    loss, lse = head.linear_xent(x, w, t)
+    check(type("R", (), {"loss": loss, "lse": lse})(), x, w, t, None, dt, v)
+
+
+@pytest.mark.parametrize("dt", list(DT))
+@pytest.mark.parametrize("skip", [0.5, 0.95, 1.0])
+def test_tokens_that_do_not_count(head, dt, skip):
+    """their rows of x may hold anything"""
+    n, v, h = 300, 500, 72
+    x, w, t = inputs(n, v, h, dt, 2, skip=skip)
+    if skip == 1.0:
+        t.fill_(IGNORE)
+    x[t == IGNORE] = float("nan")
+    x[(t == IGNORE).nonzero()[:1, 0]] = float("inf")
+    r = head.linear_xent_step(x, w, t)
+    assert torch.isfinite(r.dw).all()
+    check(r, x, w, t, None, dt, v)
+    assert not r.dx[t == IGNORE].any()
+    if skip == 1.0:
+        assert not r.dw.any() and not r.loss.any()
+    loss, lse = head.linear_xent(x, w, t)
+    assert torch.equal(loss, r.loss) and torch.equal(lse, r.lse)
+
+
+@pytest.mark.parametrize("dt", list(DT))
+@pytest.mark.parametrize("chunk", [128, 192])
+def test_chunks(head, dt, chunk):
+    """more than one chunk, the last ones partly or wholly without tokens"""
+    for n, skip in ((500, 0.0), (500, 0.4), (700, 0.9)):
+        v, h = 260, 100
+        x, w, t = inputs(n, v, h, dt, 3, skip=skip)
+        weight = torch.rand(n, device="cuda")
+        check(head.linear_xent_step(x, w, t, weight, chunk=chunk), x, w, t, weight, dt, v)
+        loss, lse = head.linear_xent(x, w, t, chunk=chunk)
+        check(type("R", (), {"loss": loss, "lse": lse})(), x, w, t, weight, dt, v)
+
+
+@pytest.mark.parametrize("dt", list(DT))
+def test_many_splits_and_pieces(head, dt):
+    """few tokens and a long vocabulary: dx is summed in many parts"""
+    n, v, h = 70, 20011, 48
+    x, w, t = inputs(n, v, h, dt, 4)
+    check(head.linear_xent_step(x, w, t), x, w, t, None, dt, v)
+
+
+@pytest.mark.parametrize("dt", list(DT))
+def test_far_logits(head, dt):
+    """logits of some hundreds: one entry holds all of the softmax, others are far below the smallest number"""
+    n, v, h = 90, 300, 64
+    x, w, t = inputs(n, v, h, dt, 5, scale=60.0)
+    check(head.linear_xent_step(x, w, t), x, w, t, None, dt, v)
+
+
+@pytest.mark.parametrize("dt", list(DT))
+def test_weights(head, dt):
+    n, v, h = 100, 200, 64
+    x, w, t = inputs(n, v, h, dt, 6)
+    weight = torch.randn(n, device="cuda") * 1e-3
+    weight[::3] = 0.0
+    check(head.linear_xent_step(x, w, t, weight), x, w, t, weight, dt, v)
+    zero = torch.zeros(n, device="cuda")
+    r = head.linear_xent_step(x, w, t, zero)
+    assert not r.dx.any() and not r.dw.any() and bool((r.loss > 0).any())
+
+
+def test_binary32_far_scales(head):
+    """the planes' scaling follows the largest magnitude"""
+    for sx, sw in ((1e-20, 1e20), (1e15, 1e-15), (1e-3, 1e-3)):
+        x, w, t = inputs(40, 100, 64, "f32", 7)
+        x, w = x * sx, w * sw
+        check(head.linear_xent_step(x, w, t), x, w, t, None, "f32", 100)
+    x, w = torch.zeros(4, 64, device="cuda"), torch.zeros(7, 64, device="cuda")
+    r = head.linear_xent_step(x, w, torch.zeros(4, dtype=torch.int64, device="cuda"))
+    assert torch.allclose(r.loss, torch.full((4,), math.log(7), device="cuda"), atol=1e-6) and not r.dx.any() and not r.dw.any()
+
+
+def test_target_outside_the_vocabulary(head, tc):
+    x, w, t = inputs(20, 30, 16, "f32", 8)
+    t[3], t[9] = 30, -5
+    r = head.linear_xent_step(x, w, t)
+    check(r, x, w, t, None, "f32", 30)
+    assert float(r.loss[3]) == 0 and not r.dx[9].any()
+    assert tc.device_errors() == tc.TC_KERR_BAD_INDEX
+    head.linear_xent(x, w, t.clamp(0, 29), ignore_index=5)
+    assert tc.device_errors() == 0
+
+
+def test_no_tokens(head):
+    x, w, t = inputs(0, 30, 16, "bf16", 9)
+    r = head.linear_xent_step(x, w, t, out=None)
+    assert r.loss.numel() == 0 and not r.dw.any()
+    assert head.linear_xent(x, w, t)[0].numel() == 0
+
+
+@pytest.mark.parametrize("dt", list(DT))
+def test_gradients_against_differences(head, dt):
+    """along random directions, differences of the 64-bit loss; through autograd"""
+    n, v, h = 40, 150, 64
+    x, w, t = inputs(n, v, h, dt, 10, skip=0.2)
+    x, w = x.contiguous().requires_grad_(), w.contiguous().requires_grad_()
+    weight = torch.rand(n, device="cuda")
+    loss, _ = head.linear_xent(x, w, t)
+    (loss * weight).sum().backward()
+
+    def total(a, b):
+        z = a @ b.t()
+        keep = t != IGNORE
+        one = torch.logsumexp(z, 1) - z.gather(1, t.clamp(min=0)[:, None])[:, 0]
+        return float((one * weight.double())[keep].sum())
+
+    xd, wd = x.detach().double(), w.detach().double()
+    for k in range(3):
+        a, b = torch.randn_like(xd), torch.randn_like(wd)
+        e = 1e-4
+        for u, p, g in ((a, 0, x.grad), (b, 1, w.grad)):
+            plus = total(xd + e * u, wd) if p == 0 else total(xd, wd + e * u)
+            minus = total(xd - e * u, wd) if p == 0 else total(xd, wd - e * u)
+            # the differences themselves are good to e^2; a random direction sees the gradient's
+            # relative error of 2 U + UD as a share of its length, six deviations
+            lim = 6 * (2 * U[dt] + UD[dt]) * float(g.double().norm()) + 1e-5
+            assert abs((plus - minus) / (2 * e) - float((g.double() * u).sum())) < lim
+
+
+def test_same_bits_again_and_on_another_stream(head):
+    x, w, t = inputs(300, 900, 64, "bf16", 11, skip=0.3)
+    a = head.linear_xent_step(x, w, t)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        b = head.linear_xent_step(x, w, t)
+    side.synchronize()
+    for p, q in zip(a, b):
+        assert torch.equal(p, q)
+
+
+def test_replays_in_a_graph(head):
+    """every replay, with eager work between, equals the eager result"""
+    x, w, t = inputs(150, 600, 64, "bf16", 12, skip=0.3)
+    x2, _, t2 = inputs(150, 600, 64, "bf16", 13, skip=0.6)
+    out = head.linear_xent_step(x, w, t)
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+    xs, ts = x.clone(), t.clone()
+    head.linear_xent_step(xs, w, ts, out=out, ws=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        head.linear_xent_step(xs, w, ts, out=out, ws=ws)
+    for k in range(4):
+        a, b = ((x, t), (x2, t2))[k % 2]
+        xs.copy_(a)
+        ts.copy_(b)
+        want = head.linear_xent_step(a, w, b)
+        graph.replay()
+        torch.cuda.synchronize()
+        for p, q in zip(out, want):
+            assert torch.equal(p, q)
