@@ -69,11 +69,12 @@ template <> struct Numerator<float> {
 };
 
 template <typename V8, int J> struct Cfg;
-// 128 tokens x 256 vocabulary entries (or 128 x 256 of another product), two
-// workgroups per compute unit: one's epilogue runs beside the other's product
-template <typename V8> struct Cfg<V8, 128> : Gemm<V8, 4, 2, 2, 2, 3> {};
-// 64 x 256 for fewer tokens
-template <typename V8> struct Cfg<V8, 64> : Gemm<V8, 2, 2, 4, 1, 4> {};
+// 256 x 256, one workgroup of 8 wavefronts per compute unit; for fewer tokens
+// 256 x 128 and 256 x 64, two of 4 wavefronts
+template <typename V8> struct Cfg<V8, 256> : Gemm<V8, 4, 2, 2, 4, 4> { static constexpr uint32_t PER_CU = 1; };
+template <typename V8> struct Cfg<V8, 128> : Gemm<V8, 4, 2, 2, 2, 3> { static constexpr uint32_t PER_CU = 2; };
+template <typename V8> struct Cfg<V8, 64> : Gemm<V8, 2, 2, 4, 1, 4> { static constexpr uint32_t PER_CU = 2; };
+uint32_t tile_tokens(uint64_t rows) { return rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
 
 // what the first kernels find out about the inputs, on the device
 struct Info {
@@ -89,6 +90,8 @@ __device__ __forceinline__ uint32_t chunk_tokens(const HeadArgs& a, uint32_t c0)
 
 // exponent that scales a binary32 operand: the largest magnitude becomes 2^14 .. 2^15
 __device__ __forceinline__ int plane_exp(uint32_t top) { return top == 0 ? 0 : 14 - ((int)(top >> 23) - 127); }
+
+constexpr float LOG2E = 1.44269504f;
 
 template <typename T>
 __device__ __forceinline__ uint16_t narrow(float v) {
@@ -151,29 +154,32 @@ __global__ __launch_bounds__(256) void k_head_zero(const HeadArgs a) {
   for (uint32_t k = threadIdx.x; k < a.h; k += 256) d[k] = R{};
 }
 
-// largest magnitude of x's listed rows, or of w
+// largest magnitude of x's listed rows, or of w (a maximum: any order gives it)
 __global__ __launch_bounds__(256) void k_head_top(const HeadArgs a, bool of_w) {
+  __shared__ uint32_t part[4];
   Info* const info = (Info*)a.info;
   const uint64_t rows = of_w ? a.v : info->count;
   uint32_t top = 0;
-  for (uint64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+  for (uint64_t r = blockIdx.x * 4u + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4u) {
     const float* p = of_w ? (const float*)a.w + r * a.ldw : (const float*)a.x + a.rows[r] * a.ldx;
-    for (uint32_t k = threadIdx.x; k < a.h; k += 256) top = max(top, __float_as_uint(p[k]) & 0x7FFFFFFFu);
+#pragma unroll 8
+    for (uint32_t k = threadIdx.x & 63u; k < a.h; k += 64) top = max(top, __float_as_uint(p[k]) & 0x7FFFFFFFu);
   }
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-  if ((threadIdx.x & 63u) == 0) atomicMax(of_w ? &info->top_w : &info->top_x, top);
+  if ((threadIdx.x & 63u) == 0) part[threadIdx.x >> 6] = top;
+  __syncthreads();
+  if (threadIdx.x == 0) atomicMax(of_w ? &info->top_w : &info->top_x, max(max(part[0], part[1]), max(part[2], part[3])));
 }
 
 // ------------------------------------------------------ operands laid out
-// 64 x 64 pieces of x (the chunk's listed rows) or w, as rows of a multiple of
-// 64 elements and transposed, zeros around them; binary32 as two planes.
+// 64 x 64 pieces of x (the chunk's listed rows) or w into blocks, by rows and
+// transposed, zeros around them; binary32 as two planes.
 template <typename T, bool OF_W>
-__global__ __launch_bounds__(256) void k_head_pack(const HeadArgs a, uint32_t c0, uint16_t* rows_out, uint16_t* cols_out,
-                                                   uint64_t cols_ld) {
+__global__ __launch_bounds__(256) void k_head_pack(const HeadArgs a, uint32_t c0, char* rows_out, char* cols_out) {
   using R = typename Elem<T>::raw;
   constexpr int PL = Type<T>::PLANES;
-  __shared__ uint16_t tile[PL][64][66];
+  __shared__ __attribute__((aligned(16))) uint16_t tile[PL][64][72];
   const Info info = *(const Info*)a.info;
   const uint32_t r0 = blockIdx.y * 64u, k0 = blockIdx.x * 64u;
   uint32_t rows = (uint32_t)a.v;
@@ -201,35 +207,29 @@ __global__ __launch_bounds__(256) void k_head_pack(const HeadArgs a, uint32_t c0
     }
   }
   __syncthreads();
+  const uint64_t rb = OF_W ? a.v_blocks : a.c_blocks, kb = OF_W ? a.k_dx : (uint32_t)(a.chunk / KSTAGE);
 #pragma unroll
-  for (int p = 0; p < PL; ++p) {
-    if (rows_out) {
-      uint16_t* o = rows_out + p * (OF_W ? a.wr_plane : a.xr_plane);
+  for (int p = 0; p < PL; ++p)
 #pragma unroll
-      for (uint32_t q = 0; q < 2; ++q) {
-        const uint32_t r = q * 32u + (threadIdx.x >> 3), k = (threadIdx.x & 7u) * 8u;
+    for (uint32_t q = 0; q < 2; ++q) {
+      // piece `u`: of block u / 64, at its place u % 64
+      const uint32_t u = q * 256u + threadIdx.x, blk = u >> 6, row = (u >> 2) & 15u, piece = (u & 3u) ^ turn(row);
+      const uint32_t m = (blk >> 1) * 16u + row, n = (blk & 1u) * 32u + piece * 8u;    // m along rows, n along k
+      if (rows_out && k0 + (blk & 1u) * 32u < a.k_logits * KSTAGE) {
+        char* o = rows_out + p * (OF_W ? a.wr_plane : a.xr_plane);
+        *reinterpret_cast<u32x4*>(o + (((k0 >> 5) + (blk & 1u)) * rb + (r0 >> 4) + (blk >> 1)) * 1024u + (u & 63u) * 16u) =
+            *reinterpret_cast<const u32x4*>(&tile[p][m][n]);
+      }
+      if (cols_out && (r0 >> 5) + (blk & 1u) < kb) {
+        char* o = cols_out + p * (OF_W ? a.wc_plane : a.xc_plane);
         uint16_t v[8];
 #pragma unroll
-        for (int z = 0; z < 8; ++z) v[z] = tile[p][r][k + z];
+        for (int z = 0; z < 8; ++z) v[z] = tile[p][n + z][m];
         u32x4 w;
         __builtin_memcpy(&w, v, 16);
-        if (r0 + r < rows) *reinterpret_cast<u32x4*>(o + (uint64_t)(r0 + r) * a.hp + k0 + k) = w;
+        *reinterpret_cast<u32x4*>(o + (((r0 >> 5) + (blk & 1u)) * (uint64_t)a.h_blocks + (k0 >> 4) + (blk >> 1)) * 1024u + (u & 63u) * 16u) = w;
       }
     }
-    if (cols_out) {
-      uint16_t* o = cols_out + p * (OF_W ? a.wc_plane : a.xc_plane);
-#pragma unroll
-      for (uint32_t q = 0; q < 2; ++q) {
-        const uint32_t k = q * 32u + (threadIdx.x >> 3), r = (threadIdx.x & 7u) * 8u;
-        uint16_t v[8];
-#pragma unroll
-        for (int z = 0; z < 8; ++z) v[z] = tile[p][r + z][k];
-        u32x4 w;
-        __builtin_memcpy(&w, v, 16);
-        if (k0 + k < a.h) *reinterpret_cast<u32x4*>(o + (uint64_t)(k0 + k) * cols_ld + r0 + r) = w;
-      }
-    }
-  }
 }
 
 // ---------------------------------------------------------------- the logits
@@ -241,10 +241,12 @@ __device__ __forceinline__ Tile tile_of(uint32_t t, uint32_t ni, uint32_t nj) {
   return {rem / width, group * 8u + rem % width};
 }
 
-// pt: softmax numerators relative to their piece's maximum
-template <typename T, int J, bool GRAD>
+// pt: softmax numerators relative to their piece's maximum, in blocks as dx's
+// product takes them (binary32: blocks of 2 KB, pieces where they are)
+template <typename T, int J, bool GRAD, bool DIRECT>
 __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_logits(const HeadArgs a, uint32_t c0) {
   using G = Cfg<typename Type<T>::V8, J>;
+  constexpr int PL = Type<T>::PLANES;
   extern __shared__ __attribute__((aligned(128))) char lds[];
   const Info info = *(const Info*)a.info;
   const uint32_t left = chunk_tokens(a, c0);
@@ -254,11 +256,16 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
   if (t >= ni * nj) return;
   const Tile tile = tile_of(t, ni, nj);
   const uint32_t i0 = tile.i * G::TI, j0 = tile.j * G::TJ;
-  const GemmOperand A{(const char*)a.wr, a.wr_ld, (uint32_t)a.v, nullptr, a.wr_plane * 2};
-  const GemmOperand B{(const char*)a.xr, a.xr_ld, left, a.xr_map ? a.rows + c0 : nullptr, a.xr_plane * 2};
+  const Blocks B{a.xr, a.c_blocks, a.xr_plane};
   f32x16 acc[G::WI][G::WJ];
-  const uint32_t per = a.k_logits;
-  G::run(A, i0, B, j0, per, 0, (Type<T>::PLANES == 2 ? 3 : 1) * per, lds, acc);
+  const uint32_t per = a.k_logits, count = (PL == 2 ? 3 : 1) * per;
+  if constexpr (DIRECT) {
+    const Rows A{(const char*)a.w, a.ldw * 2, (uint32_t)a.v, nullptr};
+    G::template run<1>(A, i0, B, j0, per, 0, count, lds, acc);
+  } else {
+    const Blocks A{a.wr, a.v_blocks, a.wr_plane};
+    G::template run<PL == 2 ? 3 : 1>(A, i0, B, j0, per, 0, count, lds, acc);
+  }
 
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h = lane >> 5;
   const uint32_t iw = i0 + (wave % G::NWI) * (G::WI * 32), jw = j0 + (wave / G::NWI) * (G::WJ * 32) + (lane & 31u);
@@ -292,18 +299,25 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
     for (int x = 0; x < G::WI; ++x) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const float p = __builtin_amdgcn_exp2f((acc[x][y][r] - top) * 1.44269504f);
+        const float p = __builtin_amdgcn_exp2f((acc[x][y][r] - top) * LOG2E);
         acc[x][y][r] = p;
         sum += p;
       }
       if (GRAD && j < left) {
-        const uint32_t i = iw + x * 32 + h * 16;
-        if (i < a.vp) {
+        const uint32_t kb = (iw >> 5) + x;
+        if (kb < a.k_dx) {
           using R = typename Numerator<T>::R;
           R v[16];
 #pragma unroll
           for (int r = 0; r < 16; ++r) v[r] = Numerator<T>::down(acc[x][y][r]);
-          store_run<R, 16>((R*)a.pt + (uint64_t)j * a.vp + i, v);
+          constexpr uint32_t PIECE = 8 * sizeof(R);
+          char* o = a.pt + ((uint64_t)kb * a.c_blocks + (j >> 4)) * (64u * PIECE) + (j & 15u) * 4u * PIECE;
+          if constexpr (PL == 2) {
+            __builtin_memcpy(o + h * 2 * PIECE, v, 2 * PIECE);
+          } else {
+            __builtin_memcpy(o + ((2u * h) ^ turn(j)) * PIECE, v, PIECE);
+            __builtin_memcpy(o + ((2u * h + 1u) ^ turn(j)) * PIECE, v + 8, PIECE);
+          }
         }
       }
     }
@@ -353,7 +367,9 @@ __global__ __launch_bounds__(SNT) void k_head_loss(const HeadArgs a, uint32_t c0
 template <typename T>
 __global__ __launch_bounds__(256) void k_head_softmax(const HeadArgs a, uint32_t c0, uint32_t piece_bits) {
   constexpr int PL = Type<T>::PLANES;
-  __shared__ uint16_t tile[PL][128][66];
+  using R = typename Numerator<T>::R;
+  constexpr uint32_t PIECE = 8 * sizeof(R);
+  __shared__ __attribute__((aligned(16))) uint16_t tile[PL][128][72];
   __shared__ float lse[64], wt[64];
   __shared__ uint32_t goal[64];
   const Info info = *(const Info*)a.info;
@@ -376,15 +392,19 @@ __global__ __launch_bounds__(256) void k_head_softmax(const HeadArgs a, uint32_t
   __syncthreads();
 #pragma unroll
   for (uint32_t q = 0; q < 2; ++q) {
-    // 16 entries of one token
-    const uint32_t r = q * 32u + (threadIdx.x >> 3), c = (threadIdx.x & 7u) * 16u, j = j0 + r, i = i0 + c;
+    // two pieces of one token: 32 such pairs in each of 16 blocks
+    const uint32_t u = q * 256u + threadIdx.x, blk = u >> 5, half = u & 1u;
+    const uint32_t r = (blk & 3u) * 16u + ((u >> 1) & 15u), c = (blk >> 2) * 32u + half * 16u, j = j0 + r, i = i0 + c;
     float p[16] = {};
-    const bool in = j < left && i < a.vp;
+    const bool in = j < left && (i >> 5) < a.k_dx;
+    const uint64_t block = (uint64_t)(i >> 5) * a.c_blocks + (j >> 4);
+    const uint32_t first = PL == 2 ? 0u : turn(j);
     if (in) {
       const float f = __expf(a.stats[(uint64_t)(i >> piece_bits) * a.chunk + j].x - lse[r]);
-      using R = typename Numerator<T>::R;
+      const char* s = a.pt + block * (64u * PIECE) + (j & 15u) * 4u * PIECE;
       R v[16];
-      load_run<R, 16>((const R*)a.pt + (uint64_t)j * a.vp + i, v);
+      __builtin_memcpy(v, s + ((2u * half) ^ first) * PIECE, PIECE);
+      __builtin_memcpy(v + 8, s + ((2u * half + 1u) ^ first) * PIECE, PIECE);
 #pragma unroll
       for (int z = 0; z < 16; ++z) p[z] = Numerator<T>::up(v[z], f);
 #pragma unroll
@@ -406,11 +426,9 @@ __global__ __launch_bounds__(256) void k_head_softmax(const HeadArgs a, uint32_t
     if (in)
 #pragma unroll
       for (int l = 0; l < PL; ++l) {
-        u32x4 w[2];
-        __builtin_memcpy(w, v[l], 32);
-        u32x4* o = reinterpret_cast<u32x4*>((uint16_t*)a.pr + l * a.pr_plane + (uint64_t)j * a.vp + i);
-        o[0] = w[0];
-        o[1] = w[1];
+        char* o = a.pr + l * a.pr_plane + block * 1024u + (j & 15u) * 64u;
+        __builtin_memcpy(o + ((2u * half) ^ turn(j)) * 16u, v[l], 16);
+        __builtin_memcpy(o + ((2u * half + 1u) ^ turn(j)) * 16u, v[l] + 8, 16);
       }
   }
   __syncthreads();
@@ -418,14 +436,12 @@ __global__ __launch_bounds__(256) void k_head_softmax(const HeadArgs a, uint32_t
   for (int l = 0; l < PL; ++l)
 #pragma unroll
     for (uint32_t q = 0; q < 4; ++q) {
-      const uint32_t c = q * 32u + (threadIdx.x >> 3), r = (threadIdx.x & 7u) * 8u;
+      // one piece of 8 tokens: 64 in each of 16 blocks
+      const uint32_t u = q * 256u + threadIdx.x, blk = u >> 6, row = (u >> 2) & 15u, piece = (u & 3u) ^ turn(row);
+      const uint32_t c = (blk >> 1) * 16u + row, r = (blk & 1u) * 32u + piece * 8u;
       if (i0 + c >= a.v) continue;
-      uint16_t v[8];
-#pragma unroll
-      for (int z = 0; z < 8; ++z) v[z] = tile[l][c][r + z];
-      u32x4 w;
-      __builtin_memcpy(&w, v, 16);
-      *reinterpret_cast<u32x4*>((uint16_t*)a.pc + l * a.pc_plane + (uint64_t)(i0 + c) * a.chunk + j0 + r) = w;
+      *reinterpret_cast<u32x4*>(a.pc + l * a.pc_plane + (((j0 >> 5) + (blk & 1u)) * (uint64_t)a.v_blocks + (i0 >> 4) + (blk >> 1)) * 1024u +
+                                (u & 63u) * 16u) = *reinterpret_cast<const u32x4*>(&tile[l][c][r]);
     }
 }
 
@@ -445,10 +461,9 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
   const uint32_t i0 = tile.i * G::TI, j0 = tile.j * G::TJ;
   const uint32_t all = (Type<T>::PLANES == 2 ? 3 : 1) * a.k_dx;
   const uint32_t s0 = (uint32_t)((uint64_t)all * split / a.splits), s1 = (uint32_t)((uint64_t)all * (split + 1) / a.splits);
-  const GemmOperand A{(const char*)a.wc, a.vp * 2, a.h, nullptr, a.wc_plane * 2};
-  const GemmOperand B{(const char*)a.pr, a.vp * 2, left, nullptr, a.pr_plane * 2};
+  const Blocks A{a.wc, a.h_blocks, a.wc_plane}, B{a.pr, a.c_blocks, a.pr_plane};
   f32x16 acc[G::WI][G::WJ];
-  G::run(A, i0, B, j0, a.k_dx, s0, s1 - s0, lds, acc);
+  G::template run<Type<T>::PLANES == 2 ? 3 : 1>(A, i0, B, j0, a.k_dx, s0, s1 - s0, lds, acc);
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h = lane >> 5;
   const uint32_t iw = i0 + (wave % G::NWI) * (G::WI * 32) + h * 16, jw = j0 + (wave / G::NWI) * (G::WJ * 32) + (lane & 31u);
 #pragma unroll
@@ -485,8 +500,8 @@ __global__ __launch_bounds__(256) void k_head_dx_sum(const HeadArgs a, uint32_t 
 // chunk's tokens.  One chunk: rounded to its dtype here.  More: binary32 sums
 // from chunk to chunk, rounded by k_head_dw_round after the last.
 template <typename T>
-__global__ __launch_bounds__((Cfg<typename Type<T>::V8, 128>::NT), 2) void k_head_dw(const HeadArgs a, uint32_t c0) {
-  using G = Cfg<typename Type<T>::V8, 128>;
+__global__ __launch_bounds__((Cfg<typename Type<T>::V8, 256>::NT), 2) void k_head_dw(const HeadArgs a, uint32_t c0) {
+  using G = Cfg<typename Type<T>::V8, 256>;
   using R = typename Elem<T>::raw;
   extern __shared__ __attribute__((aligned(128))) char lds[];
   const Info info = *(const Info*)a.info;
@@ -497,10 +512,9 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, 128>::NT), 2) void k_hea
   if (t >= ni * nj) return;
   const uint32_t i0 = t % ni * G::TI, j0 = t / ni * G::TJ;
   const uint32_t per = (left + KSTAGE - 1) / KSTAGE;
-  const GemmOperand A{(const char*)a.xc, a.chunk * 2, a.h, nullptr, a.xc_plane * 2};
-  const GemmOperand B{(const char*)a.pc, a.chunk * 2, (uint32_t)a.v, nullptr, a.pc_plane * 2};
+  const Blocks A{a.xc, a.h_blocks, a.xc_plane}, B{a.pc, a.v_blocks, a.pc_plane};
   f32x16 acc[G::WI][G::WJ];
-  G::run(A, i0, B, j0, per, 0, (Type<T>::PLANES == 2 ? 3 : 1) * per, lds, acc);
+  G::template run<Type<T>::PLANES == 2 ? 3 : 1>(A, i0, B, j0, per, 0, (Type<T>::PLANES == 2 ? 3 : 1) * per, lds, acc);
   float f = 1.0f / P_SCALE<T>;
   if (!std::is_same_v<T, bf16_t>) f *= __uint_as_float(info.top_g);
   if (Type<T>::PLANES == 2) f = __builtin_ldexpf(f, -plane_exp(info.top_x));
@@ -574,23 +588,29 @@ hipError_t chunk_of(HeadArgs& a, uint32_t c0, uint32_t rows, hipStream_t st) {
   const uint32_t ni = ((uint32_t)a.v + G::TI - 1) / G::TI;
   constexpr uint32_t PIECE = G::WI * 32;
   const uint32_t pieces = ((uint32_t)a.v + PIECE - 1) / PIECE;
-  if (a.xr_packed || GRAD) {
-    hipLaunchKernelGGL((k_head_pack<T, false>), dim3((a.h + 63) / 64, (rows + 63) / 64), dim3(256), 0, st, a, c0,
-                       a.xr_packed ? (uint16_t*)a.xr : nullptr, GRAD ? (uint16_t*)a.xc : nullptr, a.chunk);
-    HEAD_TRY(hipGetLastError());
+  hipLaunchKernelGGL((k_head_pack<T, false>), dim3((a.h + 63) / 64, (rows + 63) / 64), dim3(256), 0, st, a, c0, a.xr,
+                     GRAD ? a.xc : nullptr);
+  HEAD_TRY(hipGetLastError());
+  if constexpr (!GRAD && Type<T>::PLANES == 1) {
+    if (!a.wr) {
+      HEAD_TRY((launch_lds<k_head_logits<T, J, false, true>>(ni * nj, G::NT, G::LDS, st, a, c0)));
+    } else {
+      HEAD_TRY((launch_lds<k_head_logits<T, J, false, false>>(ni * nj, G::NT, G::LDS, st, a, c0)));
+    }
+  } else {
+    HEAD_TRY((launch_lds<k_head_logits<T, J, GRAD, false>>(ni * nj, G::NT, G::LDS, st, a, c0)));
   }
-  HEAD_TRY((launch_lds<k_head_logits<T, J, GRAD>>(ni * nj, G::NT, G::LDS, st, a, c0)));
   hipLaunchKernelGGL(k_head_loss, dim3((rows + 63) / 64), dim3(SNT), 0, st, a, c0, pieces);
   HEAD_TRY(hipGetLastError());
   if constexpr (GRAD) {
-    hipLaunchKernelGGL((k_head_softmax<T>), dim3((uint32_t)(a.vp + 127) / 128, (rows + 63) / 64), dim3(256), 0, st, a, c0,
+    hipLaunchKernelGGL((k_head_softmax<T>), dim3((uint32_t)(a.v + 127) / 128, (rows + 63) / 64), dim3(256), 0, st, a, c0,
                        PIECE == 128 ? 7u : 6u);
     HEAD_TRY(hipGetLastError());
     const uint32_t nh = (a.h + G::TI - 1) / G::TI;
     HEAD_TRY((launch_lds<k_head_dx<T, J>>(nh * nj * a.splits, G::NT, G::LDS, st, a, c0)));
     hipLaunchKernelGGL((k_head_dx_sum<T>), dim3(rows), dim3(256), 0, st, a, c0);
     HEAD_TRY(hipGetLastError());
-    using W = Cfg<typename Type<T>::V8, 128>;
+    using W = Cfg<typename Type<T>::V8, 256>;
     const uint32_t tiles = ((a.h + W::TI - 1) / W::TI) * (((uint32_t)a.v + W::TJ - 1) / W::TJ);
     HEAD_TRY((launch_lds<k_head_dw<T>>(tiles, W::NT, W::LDS, st, a, c0)));
   }
@@ -611,17 +631,18 @@ hipError_t head_of(HeadArgs& a, bool grad, hipStream_t st) {
     hipLaunchKernelGGL(k_head_top, dim3((uint32_t)std::min<uint64_t>(a.v, 2048)), dim3(256), 0, st, a, true);
     HEAD_TRY(hipGetLastError());
   }
-  if (a.wr_packed || grad) {
+  if (a.wr || grad) {
     hipLaunchKernelGGL((k_head_pack<T, true>), dim3((a.h + 63) / 64, ((uint32_t)a.v + 63) / 64), dim3(256), 0, st, a, 0u,
-                       a.wr_packed ? (uint16_t*)a.wr : nullptr, grad ? (uint16_t*)a.wc : nullptr, a.vp);
+                       a.wr, grad ? a.wc : nullptr);
     HEAD_TRY(hipGetLastError());
   }
   // (without a token one chunk still writes a dw of zeros)
   for (uint64_t c0 = 0; c0 == 0 || c0 < a.n; c0 += a.chunk) {
     const uint32_t rows = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(a.chunk, a.n - c0));
-    const bool few = rows <= 64;
-    HEAD_TRY(few ? (grad ? chunk_of<T, 64, true>(a, (uint32_t)c0, rows, st) : chunk_of<T, 64, false>(a, (uint32_t)c0, rows, st))
-                 : (grad ? chunk_of<T, 128, true>(a, (uint32_t)c0, rows, st) : chunk_of<T, 128, false>(a, (uint32_t)c0, rows, st)));
+    const uint32_t tokens = tile_tokens(rows), c = (uint32_t)c0;
+    HEAD_TRY(tokens == 64    ? (grad ? chunk_of<T, 64, true>(a, c, rows, st) : chunk_of<T, 64, false>(a, c, rows, st))
+             : tokens == 128 ? (grad ? chunk_of<T, 128, true>(a, c, rows, st) : chunk_of<T, 128, false>(a, c, rows, st))
+                             : (grad ? chunk_of<T, 256, true>(a, c, rows, st) : chunk_of<T, 256, false>(a, c, rows, st)));
   }
   if (grad && a.dw_sum) {
     hipLaunchKernelGGL((k_head_dw_round<T>), dim3((uint32_t)std::min<uint64_t>(a.v, 8192)), dim3(256), 0, st, a);
@@ -633,28 +654,28 @@ hipError_t head_of(HeadArgs& a, bool grad, hipStream_t st) {
 }  // namespace
 
 // -------------------------------------------------------------- the workspace
-// Sizes and places; `base` may be null (sizes only).  Returns the bytes.
+// Sizes and places; `base` may be null (sizes only; a null w
+// counts as one that has to be laid out).  Returns the bytes.
 uint64_t head_plan(HeadArgs& a, int dt, bool grad, char* base) {
   const uint64_t e = dt_size(dt), planes = dt == DT_F32 ? 2 : 1;
-  a.hp = (a.h + 63) / 64 * 64;
+  auto blocks = [](uint64_t rows) { return (uint32_t)((rows + 255) / 256 * 16); };
+  a.k_logits = (uint32_t)((a.h + KSTAGE - 1) / KSTAGE);
+  a.k_dx = (uint32_t)((a.v + KSTAGE - 1) / KSTAGE);
+  a.h_blocks = blocks(a.h);
+  a.v_blocks = blocks(a.v);
   a.hq = (a.h + 15) / 16 * 16;
-  a.vp = (a.v + 63) / 64 * 64;
   // per token of a chunk: the softmax by tokens and by entries, and for
   // binary32 the numerators apart (16-bit ones are replaced in place)
-  const uint64_t per_row = grad ? a.vp * (planes == 2 ? 12 : 4) : (a.v + 63) / 64 * 8;
+  const uint64_t per_row = grad ? (uint64_t)a.k_dx * KSTAGE * (planes == 2 ? 12 : 4) : (a.v + 63) / 64 * 8;
   if (a.chunk == 0) a.chunk = HEAD_CHUNK_BYTES / per_row;
   a.chunk = std::min<uint64_t>(std::max<uint64_t>(a.chunk, 128), (a.n + 64) / 64 * 64);
   a.chunk = (a.chunk + 63) / 64 * 64;
+  a.c_blocks = blocks(a.chunk);
   const bool one = a.chunk >= a.n;
-  a.k_logits = (uint32_t)((a.h + KSTAGE - 1) / KSTAGE);
-  a.k_dx = (uint32_t)((a.v + KSTAGE - 1) / KSTAGE);
-  // rows as they are: 16-byte aligned, whole stages, near enough for 32-bit offsets
-  auto direct = [&](const void* p, uint64_t ld) {
-    return planes == 1 && a.h % KSTAGE == 0 && (uintptr_t)p % 16 == 0 && ld * e % 16 == 0 && ld * e < (1u << 24);
-  };
-  a.wr_packed = !direct(a.w, a.ldw);
-  a.xr_packed = !direct(a.x, a.ldx) || a.n * a.ldx * e >= (1ull << 32);
-  a.xr_map = !a.xr_packed;
+  // the loss alone reads w as it is where its rows are 16-byte aligned, whole
+  // stages, and near enough for 32-bit offsets within a tile
+  const bool direct = !grad && planes == 1 && a.h % KSTAGE == 0 && (uintptr_t)a.w % 16 == 0 && a.ldw * e % 16 == 0 &&
+                      a.ldw * e < (1u << 24);
   uint64_t at = 0;
   auto take = [&](uint64_t bytes) {
     char* p = base ? base + at : nullptr;
@@ -666,26 +687,25 @@ uint64_t head_plan(HeadArgs& a, int dt, bool grad, char* base) {
   a.zt = (float*)take(a.chunk * 4);
   a.row_lse = (float*)take(a.chunk * 4);
   a.stats = (float2*)take((a.v + 63) / 64 * a.chunk * 8);
-  a.wr_plane = a.v * a.hp;
-  a.xr_plane = a.chunk * a.hp;
-  a.wr = a.wr_packed ? take(planes * a.wr_plane * 2) : (char*)const_cast<void*>(a.w);
-  a.xr = a.xr_packed ? take(planes * a.xr_plane * 2) : (char*)const_cast<void*>(a.x);
-  a.wr_ld = a.wr_packed ? a.hp * 2 : a.ldw * e;
-  a.xr_ld = a.xr_packed ? a.hp * 2 : a.ldx * e;
+  a.wr_plane = (uint64_t)a.v_blocks * a.k_logits * 1024;
+  a.xr_plane = (uint64_t)a.c_blocks * a.k_logits * 1024;
+  a.wr = direct ? nullptr : take(planes * a.wr_plane);
+  a.xr = take(planes * a.xr_plane);
   if (grad) {
-    a.wc_plane = a.h * a.vp;
-    a.xc_plane = a.h * a.chunk;
-    a.pr_plane = a.chunk * a.vp;
-    a.pc_plane = a.v * a.chunk;
-    a.wc = take(planes * a.wc_plane * 2);
-    a.xc = take(planes * a.xc_plane * 2);
-    a.pr = take(planes * a.pr_plane * 2);
-    a.pc = take(planes * a.pc_plane * 2);
-    a.pt = planes == 2 ? take(a.pr_plane * 4) : a.pr;
-    // enough parts of the vocabulary to give every compute unit two
+    const uint64_t kc = a.chunk / KSTAGE;
+    a.wc_plane = (uint64_t)a.h_blocks * a.k_dx * 1024;
+    a.xc_plane = (uint64_t)a.h_blocks * kc * 1024;
+    a.pr_plane = (uint64_t)a.c_blocks * a.k_dx * 1024;
+    a.pc_plane = (uint64_t)a.v_blocks * kc * 1024;
+    a.wc = take(planes * a.wc_plane);
+    a.xc = take(planes * a.xc_plane);
+    a.pr = take(planes * a.pr_plane);
+    a.pc = take(planes * a.pc_plane);
+    a.pt = planes == 2 ? take(a.pr_plane * 2) : a.pr;
+    // as many parts of the vocabulary as give every compute unit its
     // workgroups, none below 16 stages
-    const uint64_t tj = a.chunk <= 64 ? 64 : 128, tiles = (a.h + 255) / 256 * ((a.chunk + tj - 1) / tj);
-    const uint64_t stages = (planes == 2 ? 3 : 1) * (uint64_t)a.k_dx, room = 2ull * (uint64_t)device_cus();
+    const uint64_t tj = tile_tokens(a.chunk), tiles = (a.h + 255) / 256 * ((a.chunk + tj - 1) / tj);
+    const uint64_t stages = (planes == 2 ? 3 : 1) * (uint64_t)a.k_dx, room = (tj == 256 ? 1 : 2) * (uint64_t)device_cus();
     a.splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(room / std::max<uint64_t>(tiles, 1), stages / 16));
     a.dx_part = (float*)take(a.splits * a.chunk * a.hq * 4);
     a.dw_sum = one ? nullptr : (float*)take(a.v * a.hq * 4);

@@ -788,8 +788,7 @@ TC_API tc_status tc_xent_workspace_bytes(const tc_xent* c, int grad, size_t* byt
   a.ldx = c->ldx;
   a.ldw = c->ldw;
   a.chunk = c->chunk;
-  // operands that may turn out to need packing (their addresses decide): as if they did
-  a.x = a.w = (const void*)1;
+  a.w = (const void*)1;   // (its address decides whether it has to be laid out: as if it did)
   *bytes = (size_t)tc::head_plan(a, c->dt, grad != 0, nullptr);
   return TC_OK;
 }

@@ -31,14 +31,85 @@ __device__ __forceinline__ f32x16 mfma(bhalf8 a, bhalf8 b, f32x16 c) {
 constexpr uint32_t KSTAGE = 32;                 // elements of k per stage
 constexpr uint32_t ROW_BYTES = KSTAGE * 2;      // of one row in an LDS slot
 
-// One operand: row r's first element at p + r * ld bytes (16-byte aligned);
-// rows past the last one read the last one (their results are dropped).
-struct GemmOperand {
+// 16-byte piece c (of 4) of row r lies at place c ^ turn(r) of the row: the 16
+// rows that a quarter of a wavefront reads at one piece then lie in 16
+// different places of the banks.
+__device__ __forceinline__ uint32_t turn(uint32_t r) { return (r >> 2) & 3u; }
+
+// An operand that lies in memory as the LDS wants it: blocks of 16 rows by 32
+// elements, 1 KB each, pieces turned; a k stage's blocks one after the other.
+// Every load is then 1 KB in a row, from a scalar address.
+struct Blocks {
+  const char* p;
+  uint32_t rows;         // row blocks, a multiple of 16: a tile never reaches past them
+  uint64_t plane;        // bytes from the high to the low plane (binary32)
+};
+// byte of element (r, k) in an operand of `rows` row blocks
+__device__ __forceinline__ uint64_t block_byte(uint64_t r, uint64_t k, uint64_t rows) {
+  return ((k >> 5) * rows + (r >> 4)) * 1024u + (r & 15u) * 64u + ((((uint32_t)k >> 3) & 3u) ^ turn((uint32_t)r)) * 16u + ((uint32_t)k & 7u) * 2u;
+}
+
+// An operand as the caller has it: row r's first element at p + r * ld bytes
+// (16-byte aligned).  A load takes 64 bytes of 16 rows.
+struct Rows {
   const char* p;
   uint64_t ld;           // bytes from row to row, below 2^24
-  uint32_t rows;         // >= 1
+  uint32_t rows;         // >= 1; rows past the last one read the last one
   const uint32_t* map;   // or nullptr: row r is row map[r] of the memory, which then ends below 4 GiB
-  uint64_t plane;        // bytes from the high to the low plane (binary32)
+};
+
+// 16 bytes per lane from memory to 1 KB of the LDS; AT goes to either address
+template <int AT>
+__device__ __forceinline__ void load16(const char* g, char* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)g, (__attribute__((address_space(3))) void*)to, 16, AT, 0);
+}
+
+// A wavefront's L loads of one operand per stage, and the walk along k.  What
+// a stage needs in scalar instructions is counted: they are issued in order
+// with the products, and 45 of them a stage cost a third of the kernel's time.
+template <typename O, uint32_t L> struct Loader;
+template <uint32_t L> struct Loader<Blocks, L> {
+  const char* at;
+  uint64_t stage, plane;
+  uint32_t lane16;
+  __device__ __forceinline__ Loader(const Blocks& o, uint32_t row0, uint32_t wave, uint32_t k) {
+    stage = (uint64_t)o.rows * 1024u;
+    plane = o.plane;
+    lane16 = (threadIdx.x & 63u) * 16u;
+    at = o.p + (uint64_t)((row0 >> 4) + wave * L) * 1024u + k * stage;
+  }
+  __device__ __forceinline__ void go(uint32_t t, char* to) {
+    // (as a scalar base and a 32-bit offset)
+    asm volatile("" : "+v"(lane16));
+    const char* g = at + lane16;
+    static_assert(L <= 4, "offsets");
+    if (t == 0) load16<0>(g, to);
+    else if (t == 1) load16<1024>(g, to);
+    else if (t == 2) load16<2048>(g, to);
+    else load16<3072>(g, to);
+  }
+  __device__ __forceinline__ void next(bool more) { at += more ? stage : 0; }
+  // from the end of one walk over k to the start of another, in the same plane (0) or the other (+1, -1)
+  __device__ __forceinline__ void again(uint32_t per, int to) { at += (int64_t)plane * to - (int64_t)(stage * per); }
+};
+template <uint32_t L> struct Loader<Rows, L> {
+  const char* at;
+  uint32_t off[L];
+  __device__ __forceinline__ Loader(const Rows& o, uint32_t row0, uint32_t wave, uint32_t k) {
+    const uint32_t lane = threadIdx.x & 63u;
+    at = (o.map ? o.p : o.p + (uint64_t)row0 * o.ld) + (uint64_t)k * ROW_BYTES;
+#pragma unroll
+    for (uint32_t t = 0; t < L; ++t) {
+      const uint32_t r = (wave * L + t) * 16u + (lane >> 2), row = min(row0 + r, o.rows - 1u);
+      off[t] = (o.map ? o.map[row] : row - row0) * (uint32_t)o.ld + ((lane & 3u) ^ turn(r)) * 16u;
+    }
+  }
+  __device__ __forceinline__ void go(uint32_t t, char* to) {
+    asm volatile("" : "+v"(off[t]));
+    load16<0>(at + off[t], to + t * 1024u);
+  }
+  __device__ __forceinline__ void next(bool more) { at += more ? ROW_BYTES : 0; }
+  __device__ __forceinline__ void again(uint32_t, int) {}
 };
 
 template <typename V8, int WI_, int WJ_, int NWI_, int NWJ_, int NS_>
@@ -50,17 +121,16 @@ struct Gemm {
   static_assert(LA * 16 * NW == TI && LB * 16 * NW == TJ, "whole loads");
   static_assert(NS >= 3 && LDS <= 160 * 1024, "slots");
 
-  // 16-byte piece c of row r lies at piece c ^ turn(r): the 16 rows that a
-  // quarter of a wavefront reads at one piece then lie in 16 different places
-  static __device__ __forceinline__ uint32_t turn(uint32_t r) { return ((r >> 2) + 2u * (r >> 4)) & 3u; }
   // The row of A that a lane feeds in: with it the accumulators of a lane hold
   // 16 consecutive i (acc[fi][fj][r] is i = 32 fi + 16 (lane / 32) + r of the
   // wavefront's rows, j = 32 fj + lane % 32).
   static __device__ __forceinline__ uint32_t a_row(uint32_t a) { return ((a >> 2) & 1u) * 16u + (a >> 3) * 4u + (a & 3u); }
 
-  // stages [s0, s0 + count) of the walk over the plane pairs, `per` stages each
-  static __device__ __forceinline__ void run(const GemmOperand& A, uint32_t i0, const GemmOperand& B, uint32_t j0,
-                                             uint32_t per, uint32_t s0, uint32_t count, char* lds, f32x16 (&acc)[WI][WJ]) {
+  // stages [s0, s0 + count) of the walk over the pairs of planes (one, or
+  // three: high high, high low, low high), `per` stages each
+  template <int PAIRS, typename OA, typename OB>
+  static __device__ __forceinline__ void run(const OA& A, uint32_t i0, const OB& B, uint32_t j0, uint32_t per, uint32_t s0,
+                                             uint32_t count, char* lds, f32x16 (&acc)[WI][WJ]) {
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
     for (int x = 0; x < WI; ++x)
@@ -68,43 +138,35 @@ struct Gemm {
       for (int y = 0; y < WJ; ++y) acc[x][y] = f32x16{};
     if (count == 0) return;
 
-    const char* const a0 = A.map ? A.p : A.p + (uint64_t)i0 * A.ld;
-    const char* const b0 = B.map ? B.p : B.p + (uint64_t)j0 * B.ld;
-    uint32_t offa[LA], offb[LB];
-#pragma unroll
-    for (uint32_t t = 0; t < LA; ++t) {
-      const uint32_t r = (wave * LA + t) * 16u + (lane >> 2), piece = (lane & 3u) ^ turn(r);
-      const uint32_t row = min(i0 + r, A.rows - 1u);
-      offa[t] = (A.map ? A.map[row] : row - i0) * (uint32_t)A.ld + piece * 16u;
+    uint32_t pair = PAIRS > 1 ? s0 / per : 0, k = s0 - pair * per, left = count;
+    Loader<OA, LA> ga(A, i0, wave, k);
+    Loader<OB, LB> gb(B, j0, wave, k);
+    if constexpr (PAIRS > 1) {
+      if (pair == 2) ga.again(0, 1);
+      if (pair == 1) gb.again(0, 1);
     }
-#pragma unroll
-    for (uint32_t t = 0; t < LB; ++t) {
-      const uint32_t r = (wave * LB + t) * 16u + (lane >> 2), piece = (lane & 3u) ^ turn(r);
-      const uint32_t row = min(j0 + r, B.rows - 1u);
-      offb[t] = (B.map ? B.map[row] : row - j0) * (uint32_t)B.ld + piece * 16u;
-    }
-
-    // the next stage to load: past the last one it is loaded again, into a
-    // slot that nobody reads, so that every stage has the same loads out
-    uint32_t next = s0, pair = s0 / per, k = s0 - pair * per;
-    const uint32_t end = s0 + count;
-    auto load = [&](uint32_t slot) {
-      const char* ga = a0 + (pair == 2 ? A.plane : 0) + (uint64_t)k * ROW_BYTES;
-      const char* gb = b0 + (pair == 1 ? B.plane : 0) + (uint64_t)k * ROW_BYTES;
-      char* la = lds + slot * SLOT + wave * LA * 1024u;
-      char* lb = lds + slot * SLOT + TI * ROW_BYTES + wave * LB * 1024u;
-#pragma unroll
-      for (uint32_t t = 0; t < LA; ++t)
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(ga + offa[t]),
-                                         (__attribute__((address_space(3))) void*)(la + t * 1024u), 16, 0, 0);
-#pragma unroll
-      for (uint32_t t = 0; t < LB; ++t)
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(gb + offb[t]),
-                                         (__attribute__((address_space(3))) void*)(lb + t * 1024u), 16, 0, 0);
-      if (next + 1 < end) {
-        ++next;
-        if (++k == per) { k = 0; ++pair; }
+    // to the next stage; past the last one that is loaded again, into a slot
+    // that nobody reads, so that every stage has the same loads out
+    auto advance = [&] {
+      const bool more = left > 1;
+      left -= more;
+      ga.next(more);
+      gb.next(more);
+      if constexpr (PAIRS > 1) {
+        k += more;
+        if (k == per && more) {
+          k = 0;
+          ++pair;
+          ga.again(per, pair == 2 ? 1 : 0);
+          gb.again(per, pair == 1 ? 1 : -1);
+        }
       }
+    };
+    char* const la = lds + wave * LA * 1024u;
+    char* const lb = lds + TI * ROW_BYTES + wave * LB * 1024u;
+    auto load = [&](uint32_t slot, uint32_t t) {
+      if (t < LA) ga.go(t, la + slot);
+      else gb.go(t - LA, lb + slot);
     };
 
     const uint32_t wi = wave % NWI, wj = wave / NWI, l = lane & 31u, h = lane >> 5;
@@ -119,40 +181,53 @@ struct Gemm {
     }
     // (32 rows on, turn() is the same)
     struct Frags { V8 a[2][WI], b[2][WJ]; } f0, f1;
-    auto read = [&](uint32_t slot, Frags& f) {
-      const char* s = lds + slot * SLOT;
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-#pragma unroll
-        for (int x = 0; x < WI; ++x) f.a[q][x] = *reinterpret_cast<const V8*>(s + ra[q] + x * 32 * ROW_BYTES);
-#pragma unroll
-        for (int y = 0; y < WJ; ++y) f.b[q][y] = *reinterpret_cast<const V8*>(s + rb[q] + y * 32 * ROW_BYTES);
-      }
-    };
-    auto multiply = [&](const Frags& f) {
-#pragma unroll
-      for (int q = 0; q < 2; ++q)
-#pragma unroll
-        for (int x = 0; x < WI; ++x)
-#pragma unroll
-          for (int y = 0; y < WJ; ++y) acc[x][y] = mfma(f.a[q][x], f.b[q][y], acc[x][y]);
+    constexpr uint32_t READS = 2 * (WI + WJ), LOADS = LA + LB, PRODUCTS = 2 * WI * WJ;
+    auto read = [&](const char* s, Frags& f, uint32_t n) {
+      const uint32_t q = n / (WI + WJ), x = n % (WI + WJ);
+      if (x < WI) f.a[q][x] = *reinterpret_cast<const V8*>(s + ra[q] + x * 32 * ROW_BYTES);
+      else f.b[q][x - WI] = *reinterpret_cast<const V8*>(s + rb[q] + (x - WI) * 32 * ROW_BYTES);
     };
 
-    constexpr uint32_t PER_STAGE = LA + LB;
 #pragma unroll
-    for (uint32_t s = 0; s < NS - 1; ++s) load(s);
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((NS - 2) * PER_STAGE) : "memory");
-    read(0, f0);
-    uint32_t fill = NS - 1, from = 1;       // slots of the stage to load and to read
+    for (uint32_t s = 0; s < NS - 1; ++s) {
+#pragma unroll
+      for (uint32_t t = 0; t < LOADS; ++t) load(s * SLOT, t);
+      advance();
+    }
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((NS - 2) * LOADS) : "memory");
+#pragma unroll
+    for (uint32_t n = 0; n < READS; ++n) read(lds, f0, n);
+    uint32_t to = (NS - 1) * SLOT, from = SLOT;       // slots of the stage to load and to read
     auto step = [&](const Frags& now, Frags& then) {
       // the stage to read has landed for every wavefront, and every wavefront
       // has the stage before the present one in registers or behind it
-      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((NS - 3) * PER_STAGE) : "memory");
-      load(fill);
-      read(from, then);
-      multiply(now);
-      fill = fill + 1 == NS ? 0 : fill + 1;
-      from = from + 1 == NS ? 0 : from + 1;
+      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((NS - 3) * LOADS) : "memory");
+      __builtin_amdgcn_sched_barrier(0);
+      const char* s = lds + from;
+      // a read beside every product until all are out, and the loads spread
+      // over the stage: a wavefront issues in order, and 8 wavefronts' loads at
+      // once would hold up the products behind them
+#pragma unroll
+      for (uint32_t m = 0; m < PRODUCTS; ++m) {
+        const uint32_t q = m / (WI * WJ), x = m / WJ % WI, y = m % WJ;
+        acc[x][y] = mfma(now.a[q][x], now.b[q][y], acc[x][y]);
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (m < READS) {
+          read(s, then, m);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+#pragma unroll
+        for (uint32_t t = m * LOADS / PRODUCTS; t < (m + 1) * LOADS / PRODUCTS; ++t) {
+          load(to, t);
+          __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        }
+      }
+#pragma unroll
+      for (uint32_t n = PRODUCTS; n < READS; ++n) read(s, then, n);
+      advance();
+      to = to == (NS - 1) * SLOT ? 0 : to + SLOT;
+      from = from == (NS - 1) * SLOT ? 0 : from + SLOT;
+      __builtin_amdgcn_sched_barrier(0);
     };
     for (uint32_t s = 0; s < count; s += 2) {
       step(f0, f1);

@@ -174,20 +174,20 @@ struct HeadArgs {
   int64_t ignore;
   uint64_t chunk;        // tokens whose softmax is held at once (0: head_plan chooses)
   // head_plan
-  uint64_t hp, hq, vp;   // h and v rounded up: to 64, 16, 64
-  uint32_t k_logits, k_dx, splits;
-  bool wr_packed, xr_packed, xr_map;
-  uint64_t wr_ld, xr_ld;                                                       // bytes
-  uint64_t wr_plane, xr_plane, wc_plane, xc_plane, pr_plane, pc_plane;         // elements
+  uint64_t hq;           // h rounded up to 16
+  uint32_t k_logits, k_dx, splits;              // stages of 32 along h and along v; parts of dx's sum
+  uint32_t h_blocks, v_blocks, c_blocks;        // row blocks of 16, up to whole tiles
+  uint64_t wr_plane, xr_plane, wc_plane, xc_plane, pr_plane, pc_plane;         // bytes
   char* info;
   uint32_t* rows;        // [n] tokens that have a target
   float* zt;             // [chunk] logit of the target
   float* row_lse;        // [chunk]
   float2* stats;         // [pieces][chunk] maximum and sum of a piece of the vocabulary
-  char *wr, *xr;         // operands by rows: w [v][hp], x [chunk][hp] (or the call's own)
-  char *wc, *xc;         // and transposed: [h][vp], [h][chunk]
-  char *pr, *pc;         // softmax minus target: [chunk][vp], [v][chunk]
-  char* pt;              // numerators [chunk][vp] (16-bit types: pr)
+  // operands in blocks (tc_gemm.hpp), rows by summed index
+  char *wr, *xr;         // v by h (nullptr: the call's own w), tokens by h
+  char *wc, *xc;         // h by v, h by tokens
+  char *pr, *pc;         // softmax minus target: tokens by v, v by tokens
+  char* pt;              // numerators, tokens by v (16-bit types: pr)
   float* dx_part;        // [splits][chunk][hq]
   float* dw_sum;         // [v][hq], or nullptr with one chunk
 };
