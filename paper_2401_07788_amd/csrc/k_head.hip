@@ -13,13 +13,12 @@
 // sum of their exponentials; a small kernel joins the pieces.  With gradients
 // the epilogue also leaves exp(z - piece's maximum), 16 bits each, so that the
 // logits are computed once (6 n v h operations, not 8); another pass turns
-// them, now that lse is known, into the softmax minus the target, once by
-// tokens and once by vocabulary entries, the operands of the two gradient
-// products.  That matrix exists for a chunk of tokens only.
+// them in place, now that lse is known, into d, the operand of the two
+// gradient products.  d exists for a chunk of tokens only.
 //
-// All three products have the matrix units' operands contiguous in the summed
-// index, so w and x are transposed on the way (and padded where rows do not
-// start at 16 bytes).
+// w, x and d are laid out once as blocks (tc_gemm.hpp) and used from both
+// sides: dx sums over the rows of w, dw over the rows of x and d, through the
+// LDS's transposing reads.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -46,12 +45,14 @@ template <> struct Type<float> { using V8 = half8; static constexpr int PLANES =
 // 2^-38 at the least.
 template <typename T> constexpr float P_SCALE = std::is_same_v<T, bf16_t> ? 1.0f : 16384.0f;
 
-// How a softmax numerator (0 .. 1) is held between the two passes over it.
-// 16-bit types: in 16 bits, none for a sign.  bfloat16 needs the range of
+// How a softmax numerator (0 .. 1) is held between the two passes over it:
+// in binary32 for binary32 and wherever one tile holds all tokens (J = 64;
+// there the sums have too few terms to average its rounding), else in 16
+// bits, none for a sign.  bfloat16 needs the range of
 // binary32 rather than the bits: 7 exponent bits are all that a number up to 1
 // uses, 9 mantissa bits follow them.  binary16 needs the bits: 5 exponent bits
 // (2^-30, and evenly down to 2^-41) and 11 mantissa bits.
-template <typename T> struct Numerator {
+template <typename T, bool WIDE> struct Numerator {
   using R = uint16_t;
   static constexpr int SHIFT = std::is_same_v<T, bf16_t> ? 14 : 12;
   static constexpr float SCALE = std::is_same_v<T, bf16_t> ? 1.0f : 0x1p-96f;
@@ -62,11 +63,13 @@ template <typename T> struct Numerator {
     return __uint_as_float((uint32_t)u << SHIFT) * (f * (1.0f / SCALE));
   }
 };
-template <> struct Numerator<float> {
+template <typename T> struct Numerator<T, true> {
   using R = float;
   static __device__ __forceinline__ float down(float p) { return p; }
   static __device__ __forceinline__ float up(float p, float f) { return p * f; }
 };
+
+template <typename T, int J> constexpr bool WIDE = J == 64 || std::is_same_v<T, float>;
 
 template <typename V8, int J> struct Cfg;
 // 256 x 256, one workgroup of 8 wavefronts per compute unit; for fewer tokens
@@ -100,64 +103,87 @@ __device__ __forceinline__ uint16_t narrow(float v) {
 }
 
 // ------------------------------------------------- tokens that have a target
-constexpr int RNT = 1024;
+// rows: those that have one from the front, in order, the others after them.
+constexpr int RNT = 1024, RE = 8;      // threads; tokens of a thread at once
 
 __global__ __launch_bounds__(RNT) void k_head_rows(const HeadArgs a) {
-  __shared__ uint32_t part[RNT / WAVE], base;
+  __shared__ uint32_t part[RE][RNT / WAVE], tops[RNT / WAVE], all;
+  static_assert(RE * RNT / WAVE == 128, "two a lane");
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
   Info* const info = (Info*)a.info;
-  if (threadIdx.x == 0) base = 0;
-  uint32_t top = 0;
-  for (uint64_t i0 = 0; i0 < a.n; i0 += RNT) {
-    const uint64_t i = i0 + threadIdx.x;
-    bool keep = false;
-    if (i < a.n) {
-      const int64_t t = a.target[i];
-      keep = t != a.ignore;
-      if (keep && (t < 0 || (uint64_t)t >= a.v)) {
-        raise_error(KERR_BAD_INDEX);
-        keep = false;
-      }
-      if (!keep) a.loss[i] = a.lse[i] = 0.0f;
-      else if (a.weight) top = max(top, __float_as_uint(a.weight[i]) & 0x7FFFFFFFu);
+  uint32_t top = 0, kept = 0;
+  for (uint64_t i0 = 0; i0 < a.n; i0 += RNT * RE) {
+    int64_t t[RE];
+    float g[RE];
+#pragma unroll
+    for (int e = 0; e < RE; ++e) {
+      const uint64_t i = i0 + e * RNT + threadIdx.x;
+      t[e] = i < a.n ? a.target[i] : a.ignore;
+      g[e] = a.weight && i < a.n ? a.weight[i] : 1.0f;
     }
-    const uint64_t ones = __ballot(keep);
+    uint64_t ones[RE];
+    bool keep[RE];
+#pragma unroll
+    for (int e = 0; e < RE; ++e) {
+      const uint64_t i = i0 + e * RNT + threadIdx.x;
+      keep[e] = i < a.n && t[e] != a.ignore;
+      if (keep[e] && (t[e] < 0 || (uint64_t)t[e] >= a.v)) {
+        raise_error(KERR_BAD_INDEX);
+        keep[e] = false;
+      }
+      if (keep[e]) top = max(top, __float_as_uint(g[e]) & 0x7FFFFFFFu);
+      ones[e] = __ballot(keep[e]);
+    }
     __syncthreads();
-    if (lane == 0) part[wave] = (uint32_t)__popcll(ones);
+    if (lane == 0)
+#pragma unroll
+      for (int e = 0; e < RE; ++e) part[e][wave] = (uint32_t)__popcll(ones[e]);
     __syncthreads();
-    uint32_t at = base;
-    for (uint32_t k = 0; k < wave; ++k) at += part[k];
-    if (keep) a.rows[at + (uint32_t)__popcll(ones & ((1ull << lane) - 1))] = (uint32_t)i;
+    if (wave == 0) {
+      // exclusive sums over the 128 counts, two a lane
+      uint32_t* const p = &part[0][0] + 2 * lane;
+      const uint32_t x = p[0], y = p[1];
+      uint32_t sum = x + y;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t v = (uint32_t)__shfl_up((int)sum, d);
+        if (lane >= (uint32_t)d) sum += v;
+      }
+      p[0] = sum - x - y;
+      p[1] = sum - y;
+      if (lane == 63) all = sum;
+    }
     __syncthreads();
-    if (threadIdx.x == RNT - 1) base = at + (uint32_t)__popcll(ones);
+#pragma unroll
+    for (int e = 0; e < RE; ++e) {
+      const uint64_t i = i0 + e * RNT + threadIdx.x;
+      const uint32_t mine = kept + part[e][wave] + (uint32_t)__popcll(ones[e] & ((1ull << lane) - 1));   // kept tokens before token i
+      if (keep[e]) a.rows[mine] = (uint32_t)i;
+      else if (i < a.n) {
+        a.rows[(uint32_t)a.n - 1u - ((uint32_t)i - mine)] = (uint32_t)i;
+        a.loss[i] = a.lse[i] = 0.0f;
+      }
+    }
+    kept += all;
   }
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-  __syncthreads();
-  if (lane == 0) part[wave] = top;
+  if (lane == 0) tops[wave] = top;
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (uint32_t k = 0; k < RNT / WAVE; ++k) top = max(top, part[k]);
-    info->count = base;
-    info->top_g = a.weight ? top : 0x3F800000u;
+    for (uint32_t k = 0; k < RNT / WAVE; ++k) top = max(top, tops[k]);
+    info->count = kept;
+    info->top_g = top;
     info->top_x = info->top_w = 0;
   }
 }
 
-// gradients of tokens without a target are zero
-template <typename T>
-__global__ __launch_bounds__(256) void k_head_zero(const HeadArgs a) {
-  using R = typename Elem<T>::raw;
-  const int64_t t = a.target[blockIdx.x];
-  if (t != a.ignore && t >= 0 && (uint64_t)t < a.v) return;
-  R* d = (R*)a.dx + (uint64_t)blockIdx.x * a.h;
-  for (uint32_t k = threadIdx.x; k < a.h; k += 256) d[k] = R{};
-}
-
-// largest magnitude of x's listed rows, or of w (a maximum: any order gives it)
-__global__ __launch_bounds__(256) void k_head_top(const HeadArgs a, bool of_w) {
+// largest magnitude of x's listed rows (blockIdx.y 0) and of w (a maximum: any
+// order gives it)
+__global__ __launch_bounds__(256) void k_head_top(const HeadArgs a) {
   __shared__ uint32_t part[4];
   Info* const info = (Info*)a.info;
+  const bool of_w = blockIdx.y != 0;
   const uint64_t rows = of_w ? a.v : info->count;
   uint32_t top = 0;
   for (uint64_t r = blockIdx.x * 4u + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4u) {
@@ -173,63 +199,58 @@ __global__ __launch_bounds__(256) void k_head_top(const HeadArgs a, bool of_w) {
 }
 
 // ------------------------------------------------------ operands laid out
-// 64 x 64 pieces of x (the chunk's listed rows) or w into blocks, by rows and
-// transposed, zeros around them; binary32 as two planes.
+// x (the chunk's listed rows) or w into blocks, zeros past the end of a row
+// and in the rows that fill the last stage of a sum over rows; binary32 as
+// two planes.  A workgroup takes 16 rows by 512 elements, a lane a piece of 8.
+constexpr uint32_t PACK_KB = 16;
+
 template <typename T, bool OF_W>
-__global__ __launch_bounds__(256) void k_head_pack(const HeadArgs a, uint32_t c0, char* rows_out, char* cols_out) {
+__device__ __forceinline__ void pack_rows(const HeadArgs& a, uint32_t c0, uint32_t block) {
   using R = typename Elem<T>::raw;
   constexpr int PL = Type<T>::PLANES;
-  __shared__ __attribute__((aligned(16))) uint16_t tile[PL][64][72];
   const Info info = *(const Info*)a.info;
-  const uint32_t r0 = blockIdx.y * 64u, k0 = blockIdx.x * 64u;
-  uint32_t rows = (uint32_t)a.v;
-  if (!OF_W) {
-    rows = chunk_tokens(a, c0);
-    if (r0 >= rows) return;
-  }
+  const uint32_t wide = (a.k_logits + PACK_KB - 1) / PACK_KB, rb = block / wide, kb0 = block % wide * PACK_KB;
+  const uint32_t rows = OF_W ? (uint32_t)a.v : chunk_tokens(a, c0);
+  if (rb * 16u >= (rows + KSTAGE - 1) / KSTAGE * KSTAGE) return;
   const int e = PL == 2 ? plane_exp(OF_W ? info.top_w : info.top_x) : 0;
-  const uint32_t kk = threadIdx.x & 63u;
-#pragma unroll 4
-  for (uint32_t q = 0; q < 16; ++q) {
-    const uint32_t r = r0 + q * 4u + (threadIdx.x >> 6), k = k0 + kk;
-    R v{};
-    if (r < rows && k < a.h) {
-      const uint64_t row = OF_W ? r : a.rows[c0 + r];
-      v = ((const R*)(OF_W ? a.w : a.x))[row * (OF_W ? a.ldw : a.ldx) + k];
+  const uint32_t lane = threadIdx.x & 63u, row = lane >> 2, piece = (lane & 3u) ^ turn(row), r = rb * 16u + row;
+  const R* src = nullptr;
+  if (r < rows) src = (const R*)(OF_W ? a.w : a.x) + (uint64_t)(OF_W ? r : a.rows[c0 + r]) * (OF_W ? a.ldw : a.ldx);
+  struct __attribute__((packed, aligned(sizeof(R)))) Run { R v[8]; };
+#pragma unroll
+  for (uint32_t q = 0; q < PACK_KB / 4; ++q) {
+    const uint32_t kb = kb0 + q * 4u + (threadIdx.x >> 6), k = kb * 32u + piece * 8u;
+    if (kb >= a.k_logits) break;
+    Run v = {};
+    if (src) {
+      if (k + 8 <= a.h) v = *reinterpret_cast<const Run*>(src + k);
+      else
+#pragma unroll
+        for (uint32_t z = 0; z < 8; ++z)
+          if (k + z < a.h) v.v[z] = src[k + z];
     }
+    char* o = (OF_W ? a.wr : a.xr) + ((uint64_t)kb * (OF_W ? a.v_blocks : a.c_blocks) + rb) * 1024u + lane * 16u;
     if constexpr (PL == 2) {
-      const float s = __builtin_ldexpf(v, e);
-      const uint16_t hi = Elem<f16_t>::down(s);
-      tile[0][r - r0][kk] = hi;
-      tile[1][r - r0][kk] = Elem<f16_t>::down(s - Elem<f16_t>::up(hi));
+      uint16_t hi[8], lo[8];
+#pragma unroll
+      for (int z = 0; z < 8; ++z) {
+        const float s = __builtin_ldexpf(v.v[z], e);
+        hi[z] = Elem<f16_t>::down(s);
+        lo[z] = Elem<f16_t>::down(s - Elem<f16_t>::up(hi[z]));
+      }
+      __builtin_memcpy(o, hi, 16);
+      __builtin_memcpy(o + (OF_W ? a.wr_plane : a.xr_plane), lo, 16);
     } else {
-      tile[0][r - r0][kk] = v;
+      __builtin_memcpy(o, v.v, 16);
     }
   }
-  __syncthreads();
-  const uint64_t rb = OF_W ? a.v_blocks : a.c_blocks, kb = OF_W ? a.k_dx : (uint32_t)(a.chunk / KSTAGE);
-#pragma unroll
-  for (int p = 0; p < PL; ++p)
-#pragma unroll
-    for (uint32_t q = 0; q < 2; ++q) {
-      // piece `u`: of block u / 64, at its place u % 64
-      const uint32_t u = q * 256u + threadIdx.x, blk = u >> 6, row = (u >> 2) & 15u, piece = (u & 3u) ^ turn(row);
-      const uint32_t m = (blk >> 1) * 16u + row, n = (blk & 1u) * 32u + piece * 8u;    // m along rows, n along k
-      if (rows_out && k0 + (blk & 1u) * 32u < a.k_logits * KSTAGE) {
-        char* o = rows_out + p * (OF_W ? a.wr_plane : a.xr_plane);
-        *reinterpret_cast<u32x4*>(o + (((k0 >> 5) + (blk & 1u)) * rb + (r0 >> 4) + (blk >> 1)) * 1024u + (u & 63u) * 16u) =
-            *reinterpret_cast<const u32x4*>(&tile[p][m][n]);
-      }
-      if (cols_out && (r0 >> 5) + (blk & 1u) < kb) {
-        char* o = cols_out + p * (OF_W ? a.wc_plane : a.xc_plane);
-        uint16_t v[8];
-#pragma unroll
-        for (int z = 0; z < 8; ++z) v[z] = tile[p][n + z][m];
-        u32x4 w;
-        __builtin_memcpy(&w, v, 16);
-        *reinterpret_cast<u32x4*>(o + (((r0 >> 5) + (blk & 1u)) * (uint64_t)a.h_blocks + (k0 >> 4) + (blk >> 1)) * 1024u + (u & 63u) * 16u) = w;
-      }
-    }
+}
+
+// the first `of_w` workgroups lay out w, the others the chunk's tokens
+template <typename T>
+__global__ __launch_bounds__(256) void k_head_pack(const HeadArgs a, uint32_t c0, uint32_t of_w) {
+  if (blockIdx.x < of_w) pack_rows<T, true>(a, c0, blockIdx.x);
+  else pack_rows<T, false>(a, c0, blockIdx.x - of_w);
 }
 
 // ---------------------------------------------------------------- the logits
@@ -241,8 +262,8 @@ __device__ __forceinline__ Tile tile_of(uint32_t t, uint32_t ni, uint32_t nj) {
   return {rem / width, group * 8u + rem % width};
 }
 
-// pt: softmax numerators relative to their piece's maximum, in blocks as dx's
-// product takes them (binary32: blocks of 2 KB, pieces where they are)
+// pt: softmax numerators relative to their piece's maximum, in the blocks of d
+// (in binary32: blocks of 2 KB, pieces where they are)
 template <typename T, int J, bool GRAD, bool DIRECT>
 __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_logits(const HeadArgs a, uint32_t c0) {
   using G = Cfg<typename Type<T>::V8, J>;
@@ -272,6 +293,16 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
   if (iw >= a.v) return;
   const uint32_t piece = iw / (G::WI * 32);
   const float scale = Type<T>::PLANES == 2 ? __builtin_ldexpf(1.0f, -plane_exp(info.top_w) - plane_exp(info.top_x)) : 1.0f;
+  // entries past the vocabulary's end, in its last tile
+  if (iw + G::WI * 32 > a.v) {
+#pragma unroll
+    for (int y = 0; y < G::WJ; ++y)
+#pragma unroll
+      for (int x = 0; x < G::WI; ++x)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (iw + x * 32 + h * 16 + r >= a.v) acc[x][y][r] = -__builtin_inff();
+  }
 #pragma unroll
   for (int y = 0; y < G::WJ; ++y) {
     const uint32_t j = jw + y * 32;
@@ -281,7 +312,6 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         if (Type<T>::PLANES == 2) acc[x][y][r] *= scale;
-        if (iw + x * 32 + h * 16 + r >= a.v) acc[x][y][r] = -__builtin_inff();
         top = fmaxf(top, acc[x][y][r]);
       }
     top = fmaxf(top, __shfl_xor(top, 32));
@@ -294,25 +324,28 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
         for (int r = 0; r < 16; ++r)
           if (goal == x * 32 + h * 16 + r) a.zt[j] = acc[x][y][r];
     }
+    // one rounding of top * log2 e is common to the piece: it moves its part of lse by 2^-24 of top
     float sum = 0.0f;
+    const float shift = -top * LOG2E;
 #pragma unroll
     for (int x = 0; x < G::WI; ++x) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const float p = __builtin_amdgcn_exp2f((acc[x][y][r] - top) * LOG2E);
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[x][y][r], LOG2E, shift));
         acc[x][y][r] = p;
         sum += p;
       }
       if (GRAD && j < left) {
         const uint32_t kb = (iw >> 5) + x;
         if (kb < a.k_dx) {
-          using R = typename Numerator<T>::R;
+          using N = Numerator<T, WIDE<T, J>>;
+          using R = typename N::R;
           R v[16];
 #pragma unroll
-          for (int r = 0; r < 16; ++r) v[r] = Numerator<T>::down(acc[x][y][r]);
+          for (int r = 0; r < 16; ++r) v[r] = N::down(acc[x][y][r]);
           constexpr uint32_t PIECE = 8 * sizeof(R);
           char* o = a.pt + ((uint64_t)kb * a.c_blocks + (j >> 4)) * (64u * PIECE) + (j & 15u) * 4u * PIECE;
-          if constexpr (PL == 2) {
+          if constexpr (WIDE<T, J>) {
             __builtin_memcpy(o + h * 2 * PIECE, v, 2 * PIECE);
           } else {
             __builtin_memcpy(o + ((2u * h) ^ turn(j)) * PIECE, v, PIECE);
@@ -327,17 +360,19 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
 }
 
 // ------------------------------------------------- pieces joined, the losses
-constexpr int SNT = 1024;
+// and what d needs to know of a token: lse, weight (share: as a share of the
+// largest, for binary16's range) and target
+constexpr int SNT = 1024, SR = 16;     // threads, tokens of a workgroup
 
-__global__ __launch_bounds__(SNT) void k_head_loss(const HeadArgs a, uint32_t c0, uint32_t pieces) {
-  __shared__ float2 part[SNT / 64][64];
+__global__ __launch_bounds__(SNT) void k_head_loss(const HeadArgs a, uint32_t c0, uint32_t pieces, bool share) {
+  __shared__ float2 part[SNT / SR][SR];
   const uint32_t left = chunk_tokens(a, c0);
-  const uint32_t r = threadIdx.x & 63u, q = threadIdx.x >> 6, j = blockIdx.x * 64u + r;
-  if (blockIdx.x * 64u >= left) return;
+  const uint32_t r = threadIdx.x % SR, q = threadIdx.x / SR, j = blockIdx.x * SR + r;
+  if (blockIdx.x * SR >= left) return;
   float m = -__builtin_inff(), s = 0.0f;
   if (j < left) {
 #pragma unroll 4
-    for (uint32_t p = q; p < pieces; p += SNT / 64) {
+    for (uint32_t p = q; p < pieces; p += SNT / SR) {
       const float2 v = a.stats[(uint64_t)p * a.chunk + j];
       const float top = fmaxf(m, v.x);
       // (a piece whose logits are all -inf adds nothing)
@@ -347,102 +382,73 @@ __global__ __launch_bounds__(SNT) void k_head_loss(const HeadArgs a, uint32_t c0
   }
   part[q][r] = make_float2(m, s);
   __syncthreads();
-  if (q == 0 && j < left) {
-    float top = m;
-    for (int k = 1; k < SNT / 64; ++k) top = fmaxf(top, part[k][r].x);
-    float sum = 0.0f;
-    for (int k = 0; k < SNT / 64; ++k) sum += part[k][r].y * __expf(part[k][r].x - top);
-    const float lse = top + logf(sum);
-    const uint32_t i = a.rows[c0 + j];
+  // 64 parts of each token: 4 by every of 16 threads, those by their shuffles
+  const uint32_t rr = threadIdx.x / 16u, qq = threadIdx.x % 16u;
+  if (rr < SR) {
+    m = -__builtin_inff();
+    for (uint32_t k = qq; k < SNT / SR; k += 16) m = fmaxf(m, part[k][rr].x);
+    for (uint32_t d = 8; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    s = 0.0f;
+    for (uint32_t k = qq; k < SNT / SR; k += 16) s += part[k][rr].y * __expf(part[k][rr].x - m);
+    for (uint32_t d = 8; d > 0; d >>= 1) s += __shfl_xor(s, d);
+  }
+  const uint32_t jj = blockIdx.x * SR + rr;
+  if (rr < SR && qq == 0 && jj < left) {
+    const float lse = m + logf(s);
+    const uint32_t i = a.rows[c0 + jj];
     a.lse[i] = lse;
-    a.loss[i] = lse - a.zt[j];
-    a.row_lse[j] = lse;
+    a.loss[i] = lse - a.zt[jj];
+    if (a.row_info) {
+      const float g = a.weight ? a.weight[i] : 1.0f, most = __uint_as_float(((const Info*)a.info)->top_g);
+      const float weight = !share ? g : most > 0.0f ? g / most : 0.0f;
+      a.row_info[jj] = make_float4(lse, weight, __uint_as_float((uint32_t)a.target[i]), 0.0f);
+    }
   }
 }
 
-// --------------------------------------------- softmax minus target, twice
-// 64 tokens x 128 vocabulary entries.  By tokens (dx's operand): the entry
-// without the token's weight, which dx gets at its end.  By vocabulary entries
-// (dw's operand): times the weight (in binary16 as a share of the largest).
-template <typename T>
+// --------------------------------- d: softmax minus target, times the weight
+// A workgroup takes 128 tokens by 256 vocabulary entries, a lane half a row of
+// a block (32 bytes) at a time: one pass over the memory, bound by it.
+constexpr uint32_t SOFT_KB = 8;
+
+template <typename T, int J>
 __global__ __launch_bounds__(256) void k_head_softmax(const HeadArgs a, uint32_t c0, uint32_t piece_bits) {
   constexpr int PL = Type<T>::PLANES;
-  using R = typename Numerator<T>::R;
-  constexpr uint32_t PIECE = 8 * sizeof(R);
-  __shared__ __attribute__((aligned(16))) uint16_t tile[PL][128][72];
-  __shared__ float lse[64], wt[64];
-  __shared__ uint32_t goal[64];
-  const Info info = *(const Info*)a.info;
-  const uint32_t left = chunk_tokens(a, c0);
-  const uint32_t j0 = blockIdx.y * 64u, i0 = blockIdx.x * 128u;
-  if (j0 >= left) return;
-  if (threadIdx.x < 64) {
-    const uint32_t j = j0 + threadIdx.x;
-    lse[threadIdx.x] = 0.0f;
-    wt[threadIdx.x] = 0.0f;
-    goal[threadIdx.x] = ~0u;
-    if (j < left) {
-      const uint32_t i = a.rows[c0 + j];
-      lse[threadIdx.x] = a.row_lse[j];
-      const float g = a.weight ? a.weight[i] : 1.0f, top = __uint_as_float(info.top_g);
-      wt[threadIdx.x] = std::is_same_v<T, bf16_t> ? g : top > 0.0f ? g / top : 0.0f;
-      goal[threadIdx.x] = (uint32_t)a.target[i];
-    }
-  }
-  __syncthreads();
-#pragma unroll
-  for (uint32_t q = 0; q < 2; ++q) {
-    // two pieces of one token: 32 such pairs in each of 16 blocks
-    const uint32_t u = q * 256u + threadIdx.x, blk = u >> 5, half = u & 1u;
-    const uint32_t r = (blk & 3u) * 16u + ((u >> 1) & 15u), c = (blk >> 2) * 32u + half * 16u, j = j0 + r, i = i0 + c;
-    float p[16] = {};
-    const bool in = j < left && (i >> 5) < a.k_dx;
-    const uint64_t block = (uint64_t)(i >> 5) * a.c_blocks + (j >> 4);
-    const uint32_t first = PL == 2 ? 0u : turn(j);
+  using N = Numerator<T, WIDE<T, J>>;
+  using R = typename N::R;
+  const uint32_t left = chunk_tokens(a, c0), j = blockIdx.y * 128u + (threadIdx.x >> 1), half = threadIdx.x & 1u;
+  // (rows that fill the last stage of the sum over tokens are zeros)
+  if (j >= (left + KSTAGE - 1) / KSTAGE * KSTAGE) return;
+  const bool in = j < left;
+  const float4 row = in ? a.row_info[j] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  const uint32_t goal = __float_as_uint(row.z);
+  const float w = row.y * P_SCALE<T>;
+#pragma unroll 2
+  for (uint32_t kb = blockIdx.x * SOFT_KB; kb < min(a.k_dx, blockIdx.x * SOFT_KB + SOFT_KB); ++kb) {
+    const uint64_t at = ((uint64_t)kb * a.c_blocks + (j >> 4)) * 64u + (j & 15u) * 4u;    // in pieces
+    uint16_t v[PL][16] = {};
     if (in) {
-      const float f = __expf(a.stats[(uint64_t)(i >> piece_bits) * a.chunk + j].x - lse[r]);
-      const char* s = a.pt + block * (64u * PIECE) + (j & 15u) * 4u * PIECE;
-      R v[16];
-      __builtin_memcpy(v, s + ((2u * half) ^ first) * PIECE, PIECE);
-      __builtin_memcpy(v + 8, s + ((2u * half + 1u) ^ first) * PIECE, PIECE);
+      const float f = __expf(a.stats[(uint64_t)((kb * 32u) >> piece_bits) * a.chunk + j].x - row.x);
 #pragma unroll
-      for (int z = 0; z < 16; ++z) p[z] = Numerator<T>::up(v[z], f);
+      for (uint32_t z = 0; z < 2; ++z) {
+        const uint32_t place = 2u * half + z, piece = place ^ turn(j);
+        R n[8];
+        __builtin_memcpy(n, a.pt + (at + (WIDE<T, J> ? piece : place)) * sizeof(n), sizeof(n));
 #pragma unroll
-      for (int z = 0; z < 16; ++z)
-        if (i + z == goal[r]) p[z] -= 1.0f;
-    }
-    uint16_t v[PL][16];
-#pragma unroll
-    for (int z = 0; z < 16; ++z) {
-      const float s = p[z] * P_SCALE<T>, t = s * wt[r];
-      v[0][z] = narrow<T>(s);
-      const uint16_t hi = narrow<T>(t);
-      tile[0][c + z][r] = hi;
-      if constexpr (PL == 2) {
-        v[1][z] = narrow<T>(s - Elem<f16_t>::up(v[0][z]));
-        tile[1][c + z][r] = narrow<T>(t - Elem<f16_t>::up(hi));
+        for (uint32_t y = 0; y < 8; ++y) {
+          const bool hot = kb * 32u + piece * 8u + y == goal;
+          const float p = (N::up(n[y], f) - (hot ? 1.0f : 0.0f)) * w;
+          const uint16_t hi = narrow<T>(p);
+          v[0][z * 8 + y] = hi;
+          // (the largest entry of most tokens: dx adds what its rounding took)
+          if (PL == 1 && hot) a.rest[j] = p - Elem<T>::up(hi);
+          if constexpr (PL == 2) v[1][z * 8 + y] = narrow<T>(p - Elem<f16_t>::up(hi));
+        }
       }
     }
-    if (in)
 #pragma unroll
-      for (int l = 0; l < PL; ++l) {
-        char* o = a.pr + l * a.pr_plane + block * 1024u + (j & 15u) * 64u;
-        __builtin_memcpy(o + ((2u * half) ^ turn(j)) * 16u, v[l], 16);
-        __builtin_memcpy(o + ((2u * half + 1u) ^ turn(j)) * 16u, v[l] + 8, 16);
-      }
+    for (int l = 0; l < PL; ++l) __builtin_memcpy(a.pr + l * a.pr_plane + (at + 2u * half) * 16u, v[l], 32);
   }
-  __syncthreads();
-#pragma unroll
-  for (int l = 0; l < PL; ++l)
-#pragma unroll
-    for (uint32_t q = 0; q < 4; ++q) {
-      // one piece of 8 tokens: 64 in each of 16 blocks
-      const uint32_t u = q * 256u + threadIdx.x, blk = u >> 6, row = (u >> 2) & 15u, piece = (u & 3u) ^ turn(row);
-      const uint32_t c = (blk >> 1) * 16u + row, r = (blk & 1u) * 32u + piece * 8u;
-      if (i0 + c >= a.v) continue;
-      *reinterpret_cast<u32x4*>(a.pc + l * a.pc_plane + (((j0 >> 5) + (blk & 1u)) * (uint64_t)a.v_blocks + (i0 >> 4) + (blk >> 1)) * 1024u +
-                                (u & 63u) * 16u) = *reinterpret_cast<const u32x4*>(&tile[l][c][r]);
-    }
 }
 
 // ------------------------------------------------------------- the gradients
@@ -461,7 +467,8 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
   const uint32_t i0 = tile.i * G::TI, j0 = tile.j * G::TJ;
   const uint32_t all = (Type<T>::PLANES == 2 ? 3 : 1) * a.k_dx;
   const uint32_t s0 = (uint32_t)((uint64_t)all * split / a.splits), s1 = (uint32_t)((uint64_t)all * (split + 1) / a.splits);
-  const Blocks A{a.wc, a.h_blocks, a.wc_plane}, B{a.pr, a.c_blocks, a.pr_plane};
+  const BlocksT A{a.wr, a.v_blocks, a.wr_plane};
+  const Blocks B{a.pr, a.c_blocks, a.pr_plane};
   f32x16 acc[G::WI][G::WJ];
   G::template run<Type<T>::PLANES == 2 ? 3 : 1>(A, i0, B, j0, a.k_dx, s0, s1 - s0, lds, acc);
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h = lane >> 5;
@@ -479,19 +486,29 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
     }
 }
 
+// dx of the list's places c0 + blockIdx.x: the parts' sum, and what the target's entry of d lost when it was rounded:
+// for a token that the model is sure of, dx is a small difference and that
+// entry's rounding would be most of its error.
 template <typename T>
 __global__ __launch_bounds__(256) void k_head_dx_sum(const HeadArgs a, uint32_t c0) {
   using R = typename Elem<T>::raw;
   const Info info = *(const Info*)a.info;
-  const uint32_t j = blockIdx.x;
-  if (c0 + j >= info.count) return;
-  const uint32_t i = a.rows[c0 + j];
-  float f = (a.weight ? a.weight[i] : 1.0f) / P_SCALE<T>;
-  if (Type<T>::PLANES == 2) f = __builtin_ldexpf(f, -plane_exp(info.top_w));
+  const uint32_t j = blockIdx.x, i = a.rows[c0 + j];
   R* o = (R*)a.dx + (uint64_t)i * a.h;
+  if (c0 + j >= info.count) {
+    // (a token without a target)
+    for (uint32_t k = threadIdx.x; k < a.h; k += 256) o[k] = R{};
+    return;
+  }
+  float f = 1.0f / P_SCALE<T>;
+  if (!std::is_same_v<T, bf16_t>) f *= __uint_as_float(info.top_g);
+  if (Type<T>::PLANES == 2) f = __builtin_ldexpf(f, -plane_exp(info.top_w));
+  const float rest = Type<T>::PLANES == 1 ? a.rest[j] : 0.0f;
+  const R* w = (const R*)a.w + (uint64_t)a.target[i] * a.ldw;
   for (uint32_t k = threadIdx.x; k < a.h; k += 256) {
     float s = 0.0f;
     for (uint32_t q = 0; q < a.splits; ++q) s += a.dx_part[((uint64_t)q * a.chunk + j) * a.hq + k];
+    if (Type<T>::PLANES == 1) s += rest * Elem<T>::up(w[k]);
     o[k] = Elem<T>::down(s * f);
   }
 }
@@ -512,7 +529,7 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, 256>::NT), 2) void k_hea
   if (t >= ni * nj) return;
   const uint32_t i0 = t % ni * G::TI, j0 = t / ni * G::TJ;
   const uint32_t per = (left + KSTAGE - 1) / KSTAGE;
-  const Blocks A{a.xc, a.h_blocks, a.xc_plane}, B{a.pc, a.v_blocks, a.pc_plane};
+  const BlocksT A{a.xr, a.c_blocks, a.xr_plane}, B{a.pr, a.c_blocks, a.pr_plane};
   f32x16 acc[G::WI][G::WJ];
   G::template run<Type<T>::PLANES == 2 ? 3 : 1>(A, i0, B, j0, per, 0, (Type<T>::PLANES == 2 ? 3 : 1) * per, lds, acc);
   float f = 1.0f / P_SCALE<T>;
@@ -588,8 +605,8 @@ hipError_t chunk_of(HeadArgs& a, uint32_t c0, uint32_t rows, hipStream_t st) {
   const uint32_t ni = ((uint32_t)a.v + G::TI - 1) / G::TI;
   constexpr uint32_t PIECE = G::WI * 32;
   const uint32_t pieces = ((uint32_t)a.v + PIECE - 1) / PIECE;
-  hipLaunchKernelGGL((k_head_pack<T, false>), dim3((a.h + 63) / 64, (rows + 63) / 64), dim3(256), 0, st, a, c0, a.xr,
-                     GRAD ? a.xc : nullptr);
+  const uint32_t wide = (a.k_logits + PACK_KB - 1) / PACK_KB, of_w = a.wr && c0 == 0 ? a.k_dx * 2 * wide : 0;
+  hipLaunchKernelGGL((k_head_pack<T>), dim3(of_w + (rows + 31) / 32 * 2 * wide), dim3(256), 0, st, a, c0, of_w);
   HEAD_TRY(hipGetLastError());
   if constexpr (!GRAD && Type<T>::PLANES == 1) {
     if (!a.wr) {
@@ -600,16 +617,19 @@ hipError_t chunk_of(HeadArgs& a, uint32_t c0, uint32_t rows, hipStream_t st) {
   } else {
     HEAD_TRY((launch_lds<k_head_logits<T, J, GRAD, false>>(ni * nj, G::NT, G::LDS, st, a, c0)));
   }
-  hipLaunchKernelGGL(k_head_loss, dim3((rows + 63) / 64), dim3(SNT), 0, st, a, c0, pieces);
+  hipLaunchKernelGGL(k_head_loss, dim3((rows + SR - 1) / SR), dim3(SNT), 0, st, a, c0, pieces,
+                     !std::is_same_v<T, bf16_t>);
   HEAD_TRY(hipGetLastError());
   if constexpr (GRAD) {
-    hipLaunchKernelGGL((k_head_softmax<T>), dim3((uint32_t)(a.v + 127) / 128, (rows + 63) / 64), dim3(256), 0, st, a, c0,
+    hipLaunchKernelGGL((k_head_softmax<T, J>), dim3((a.k_dx + SOFT_KB - 1) / SOFT_KB, (rows + 127) / 128), dim3(256), 0, st, a, c0,
                        PIECE == 128 ? 7u : 6u);
     HEAD_TRY(hipGetLastError());
     const uint32_t nh = (a.h + G::TI - 1) / G::TI;
     HEAD_TRY((launch_lds<k_head_dx<T, J>>(nh * nj * a.splits, G::NT, G::LDS, st, a, c0)));
-    hipLaunchKernelGGL((k_head_dx_sum<T>), dim3(rows), dim3(256), 0, st, a, c0);
-    HEAD_TRY(hipGetLastError());
+    if (a.n > 0) {
+      hipLaunchKernelGGL((k_head_dx_sum<T>), dim3(rows), dim3(256), 0, st, a, c0);
+      HEAD_TRY(hipGetLastError());
+    }
     using W = Cfg<typename Type<T>::V8, 256>;
     const uint32_t tiles = ((a.h + W::TI - 1) / W::TI) * (((uint32_t)a.v + W::TJ - 1) / W::TJ);
     HEAD_TRY((launch_lds<k_head_dw<T>>(tiles, W::NT, W::LDS, st, a, c0)));
@@ -621,25 +641,15 @@ template <typename T>
 hipError_t head_of(HeadArgs& a, bool grad, hipStream_t st) {
   hipLaunchKernelGGL(k_head_rows, dim3(1), dim3(RNT), 0, st, a);
   HEAD_TRY(hipGetLastError());
-  if (grad && a.n > 0) {
-    hipLaunchKernelGGL((k_head_zero<T>), dim3((uint32_t)a.n), dim3(256), 0, st, a);
-    HEAD_TRY(hipGetLastError());
-  }
   if (Type<T>::PLANES == 2) {
-    hipLaunchKernelGGL(k_head_top, dim3((uint32_t)std::min<uint64_t>(a.n + 1, 2048)), dim3(256), 0, st, a, false);
-    HEAD_TRY(hipGetLastError());
-    hipLaunchKernelGGL(k_head_top, dim3((uint32_t)std::min<uint64_t>(a.v, 2048)), dim3(256), 0, st, a, true);
-    HEAD_TRY(hipGetLastError());
-  }
-  if (a.wr || grad) {
-    hipLaunchKernelGGL((k_head_pack<T, true>), dim3((a.h + 63) / 64, ((uint32_t)a.v + 63) / 64), dim3(256), 0, st, a, 0u,
-                       a.wr, grad ? a.wc : nullptr);
+    hipLaunchKernelGGL(k_head_top, dim3(512, 2), dim3(256), 0, st, a);
     HEAD_TRY(hipGetLastError());
   }
   // (without a token one chunk still writes a dw of zeros)
   for (uint64_t c0 = 0; c0 == 0 || c0 < a.n; c0 += a.chunk) {
     const uint32_t rows = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(a.chunk, a.n - c0));
-    const uint32_t tokens = tile_tokens(rows), c = (uint32_t)c0;
+    // (one choice for every chunk: the buffers go by it)
+    const uint32_t tokens = tile_tokens(a.chunk), c = (uint32_t)c0;
     HEAD_TRY(tokens == 64    ? (grad ? chunk_of<T, 64, true>(a, c, rows, st) : chunk_of<T, 64, false>(a, c, rows, st))
              : tokens == 128 ? (grad ? chunk_of<T, 128, true>(a, c, rows, st) : chunk_of<T, 128, false>(a, c, rows, st))
                              : (grad ? chunk_of<T, 256, true>(a, c, rows, st) : chunk_of<T, 256, false>(a, c, rows, st)));
@@ -661,12 +671,11 @@ uint64_t head_plan(HeadArgs& a, int dt, bool grad, char* base) {
   auto blocks = [](uint64_t rows) { return (uint32_t)((rows + 255) / 256 * 16); };
   a.k_logits = (uint32_t)((a.h + KSTAGE - 1) / KSTAGE);
   a.k_dx = (uint32_t)((a.v + KSTAGE - 1) / KSTAGE);
-  a.h_blocks = blocks(a.h);
   a.v_blocks = blocks(a.v);
   a.hq = (a.h + 15) / 16 * 16;
-  // per token of a chunk: the softmax by tokens and by entries, and for
-  // binary32 the numerators apart (16-bit ones are replaced in place)
-  const uint64_t per_row = grad ? (uint64_t)a.k_dx * KSTAGE * (planes == 2 ? 12 : 4) : (a.v + 63) / 64 * 8;
+  // per token of a chunk: d, and binary32 numerators apart (16-bit ones are
+  // replaced in place)
+  const uint64_t per_row = grad ? (uint64_t)a.k_dx * KSTAGE * (planes == 2 ? 8 : 2) : (a.v + 63) / 64 * 8;
   if (a.chunk == 0) a.chunk = HEAD_CHUNK_BYTES / per_row;
   a.chunk = std::min<uint64_t>(std::max<uint64_t>(a.chunk, 128), (a.n + 64) / 64 * 64);
   a.chunk = (a.chunk + 63) / 64 * 64;
@@ -685,23 +694,19 @@ uint64_t head_plan(HeadArgs& a, int dt, bool grad, char* base) {
   a.info = take(sizeof(Info));
   a.rows = (uint32_t*)take(a.n * 4);
   a.zt = (float*)take(a.chunk * 4);
-  a.row_lse = (float*)take(a.chunk * 4);
   a.stats = (float2*)take((a.v + 63) / 64 * a.chunk * 8);
-  a.wr_plane = (uint64_t)a.v_blocks * a.k_logits * 1024;
-  a.xr_plane = (uint64_t)a.c_blocks * a.k_logits * 1024;
+  // (a tile of 256 rows of the transposed operand: 8 blocks along k)
+  const uint64_t kh = (a.k_logits + 7) / 8 * 8, kv = (a.k_dx + 7) / 8 * 8;
+  a.wr_plane = a.v_blocks * kh * 1024;
+  a.xr_plane = a.c_blocks * kh * 1024;
   a.wr = direct ? nullptr : take(planes * a.wr_plane);
   a.xr = take(planes * a.xr_plane);
   if (grad) {
-    const uint64_t kc = a.chunk / KSTAGE;
-    a.wc_plane = (uint64_t)a.h_blocks * a.k_dx * 1024;
-    a.xc_plane = (uint64_t)a.h_blocks * kc * 1024;
-    a.pr_plane = (uint64_t)a.c_blocks * a.k_dx * 1024;
-    a.pc_plane = (uint64_t)a.v_blocks * kc * 1024;
-    a.wc = take(planes * a.wc_plane);
-    a.xc = take(planes * a.xc_plane);
+    a.pr_plane = a.c_blocks * kv * 1024;
     a.pr = take(planes * a.pr_plane);
-    a.pc = take(planes * a.pc_plane);
-    a.pt = planes == 2 ? take(a.pr_plane * 2) : a.pr;
+    a.pt = planes == 2 || a.chunk <= 64 ? take(a.pr_plane * 2) : a.pr;
+    a.row_info = (float4*)take(a.chunk * 16);
+    a.rest = (float*)take(a.chunk * 4);
     // as many parts of the vocabulary as give every compute unit its
     // workgroups, none below 16 stages
     const uint64_t tj = tile_tokens(a.chunk), tiles = (a.h + 255) / 256 * ((a.chunk + tj - 1) / tj);

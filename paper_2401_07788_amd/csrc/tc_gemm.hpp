@@ -44,11 +44,15 @@ struct Blocks {
   uint32_t rows;         // row blocks, a multiple of 16: a tile never reaches past them
   uint64_t plane;        // bytes from the high to the low plane (binary32)
 };
-// byte of element (r, k) in an operand of `rows` row blocks
-__device__ __forceinline__ uint64_t block_byte(uint64_t r, uint64_t k, uint64_t rows) {
-  return ((k >> 5) * rows + (r >> 4)) * 1024u + (r & 15u) * 64u + ((((uint32_t)k >> 3) & 3u) ^ turn((uint32_t)r)) * 16u + ((uint32_t)k & 7u) * 2u;
-}
-
+// The same memory seen from the other side: what its blocks call k are the
+// operand's rows, and the sum runs along its rows (two row blocks to a
+// stage).  The LDS gives such an operand to the matrix units by its
+// transposing reads, so that no transposed copy is made of anything.
+struct BlocksT {
+  const char* p;
+  uint32_t rows;         // row blocks of the memory
+  uint64_t plane;
+};
 // An operand as the caller has it: row r's first element at p + r * ld bytes
 // (16-byte aligned).  A load takes 64 bytes of 16 rows.
 struct Rows {
@@ -62,6 +66,15 @@ struct Rows {
 template <int AT>
 __device__ __forceinline__ void load16(const char* g, char* to) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)g, (__attribute__((address_space(3))) void*)to, 16, AT, 0);
+}
+
+// A transposing read.  Nothing else writes *p while this function runs, and
+// saying so spares it a wait for every load to the LDS that is under way (the
+// stages' own waits order them).
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef short short8v __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ short4v read_tr(__attribute__((address_space(3))) short4v* __restrict__ p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(p);
 }
 
 // A wavefront's L loads of one operand per stage, and the walk along k.  What
@@ -92,6 +105,28 @@ template <uint32_t L> struct Loader<Blocks, L> {
   // from the end of one walk over k to the start of another, in the same plane (0) or the other (+1, -1)
   __device__ __forceinline__ void again(uint32_t per, int to) { at += (int64_t)plane * to - (int64_t)(stage * per); }
 };
+template <uint32_t L> struct Loader<BlocksT, L> {
+  const char* at;
+  uint64_t plane;
+  uint32_t pitch, lane16;
+  __device__ __forceinline__ Loader(const BlocksT& o, uint32_t row0, uint32_t wave, uint32_t k) {
+    // load b of the stage is block (b & 1) along the sum, 32 rows from row0 + 32 (b >> 1) on
+    const uint32_t b = wave * L;
+    pitch = o.rows * 1024u;
+    plane = o.plane;
+    lane16 = (threadIdx.x & 63u) * 16u;
+    at = o.p + (uint64_t)((row0 >> 5) + (b >> 1)) * pitch + (2u * k + (b & 1u)) * 1024u;
+  }
+  __device__ __forceinline__ void go(uint32_t t, char* to) {
+    asm volatile("" : "+v"(lane16));
+    const char* g = at + (t >= 2 ? pitch : 0u) + lane16;
+    static_assert(L == 1 || L == 2 || L == 4, "pairs of blocks");
+    if (t & 1) load16<1024>(g, to + (t & 2) * 1024u);
+    else load16<0>(g, to + (t & 2) * 1024u);
+  }
+  __device__ __forceinline__ void next(bool more) { at += more ? 2048 : 0; }
+  __device__ __forceinline__ void again(uint32_t per, int to) { at += (int64_t)plane * to - (int64_t)(2048u * per); }
+};
 template <uint32_t L> struct Loader<Rows, L> {
   const char* at;
   uint32_t off[L];
@@ -121,10 +156,45 @@ struct Gemm {
   static_assert(LA * 16 * NW == TI && LB * 16 * NW == TJ, "whole loads");
   static_assert(NS >= 3 && LDS <= 160 * 1024, "slots");
 
-  // The row of A that a lane feeds in: with it the accumulators of a lane hold
-  // 16 consecutive i (acc[fi][fj][r] is i = 32 fi + 16 (lane / 32) + r of the
-  // wavefront's rows, j = 32 fj + lane % 32).
+  // A wavefront's fragments of one operand: get(stage's operand, k step of 16,
+  // fragment).  A lane feeds in 8 consecutive k of one row.  IS_A: of row
+  // a_row(lane), with which the accumulators of a lane hold 16 consecutive i
+  // (acc[fi][fj][r] is i = 32 fi + 16 (lane / 32) + r of the wavefront's rows,
+  // j = 32 fj + lane % 32).
   static __device__ __forceinline__ uint32_t a_row(uint32_t a) { return ((a >> 2) & 1u) * 16u + (a >> 3) * 4u + (a & 3u); }
+  template <typename O, bool IS_A> struct Reader {
+    static constexpr int READS = 1;
+    uint32_t at[2];
+    __device__ __forceinline__ Reader(uint32_t first) {
+      const uint32_t l = threadIdx.x & 31u, h = (threadIdx.x >> 5) & 1u, r = IS_A ? a_row(l) : l;
+      // (32 rows on, turn() is the same)
+#pragma unroll
+      for (uint32_t q = 0; q < 2; ++q) at[q] = (first * 32u + r) * ROW_BYTES + ((2u * q + h) ^ turn(r)) * 16u;
+    }
+    __device__ __forceinline__ V8 get(const char* s, uint32_t q, uint32_t x) const {
+      return *reinterpret_cast<const V8*>(s + at[q] + x * 32u * ROW_BYTES);
+    }
+  };
+  // Transposing reads: 16 lanes put in 4 rows (of the sum) of 4 pieces of 4
+  // elements, lane l of them gets element l of every row.
+  template <bool IS_A> struct Reader<BlocksT, IS_A> {
+    static constexpr int READS = 2;
+    uint32_t at[2];
+    __device__ __forceinline__ Reader(uint32_t first) {
+      const uint32_t lane = threadIdx.x & 63u, a = lane >> 2 & 7u;      // a: which 4 of the fragment's 32 rows
+      const uint32_t group = (a & 4u) | (lane & 3u), n = IS_A ? a_row(group * 4u) : group * 4u;
+#pragma unroll
+      for (uint32_t p = 0; p < 2; ++p) {
+        const uint32_t k = (lane >> 5) * 8u + p * 4u + ((lane >> 2) & 3u);
+        at[p] = first * 2048u + k * ROW_BYTES + ((n >> 3) ^ turn(k)) * 16u + (n & 7u) * 2u;
+      }
+    }
+    __device__ __forceinline__ V8 get(const char* s, uint32_t q, uint32_t x) const {
+      using P = __attribute__((address_space(3))) short4v*;
+      const short4v lo = read_tr((P)(s + at[0] + x * 2048u + q * 1024u)), hi = read_tr((P)(s + at[1] + x * 2048u + q * 1024u));
+      return __builtin_bit_cast(V8, (short8v)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  };
 
   // stages [s0, s0 + count) of the walk over the pairs of planes (one, or
   // three: high high, high low, low high), `per` stages each
@@ -169,23 +239,15 @@ struct Gemm {
       else gb.go(t - LA, lb + slot);
     };
 
-    const uint32_t wi = wave % NWI, wj = wave / NWI, l = lane & 31u, h = lane >> 5;
-    uint32_t ra[2], rb[2];     // this lane's piece of k step 0 and 1 in the first fragment
-    {
-      const uint32_t ar = a_row(l);
-#pragma unroll
-      for (uint32_t q = 0; q < 2; ++q) {
-        ra[q] = (wi * WI * 32u + ar) * ROW_BYTES + (((2u * q + h) ^ turn(ar)) * 16u);
-        rb[q] = TI * ROW_BYTES + (wj * WJ * 32u + l) * ROW_BYTES + (((2u * q + h) ^ turn(l)) * 16u);
-      }
-    }
-    // (32 rows on, turn() is the same)
+    const uint32_t wi = wave % NWI, wj = wave / NWI;
+    const Reader<OA, true> qa(wi * WI);
+    const Reader<OB, false> qb(wj * WJ);
     struct Frags { V8 a[2][WI], b[2][WJ]; } f0, f1;
     constexpr uint32_t READS = 2 * (WI + WJ), LOADS = LA + LB, PRODUCTS = 2 * WI * WJ;
     auto read = [&](const char* s, Frags& f, uint32_t n) {
       const uint32_t q = n / (WI + WJ), x = n % (WI + WJ);
-      if (x < WI) f.a[q][x] = *reinterpret_cast<const V8*>(s + ra[q] + x * 32 * ROW_BYTES);
-      else f.b[q][x - WI] = *reinterpret_cast<const V8*>(s + rb[q] + (x - WI) * 32 * ROW_BYTES);
+      if (x < WI) f.a[q][x] = qa.get(s, q, x);
+      else f.b[q][x - WI] = qb.get(s + TI * ROW_BYTES, q, x - WI);
     };
 
 #pragma unroll
@@ -214,7 +276,8 @@ struct Gemm {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         if (m < READS) {
           read(s, then, m);
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          if (m % (WI + WJ) < WI) __builtin_amdgcn_sched_group_barrier(0x100, Reader<OA, true>::READS, 0);
+          else __builtin_amdgcn_sched_group_barrier(0x100, Reader<OB, false>::READS, 0);
         }
 #pragma unroll
         for (uint32_t t = m * LOADS / PRODUCTS; t < (m + 1) * LOADS / PRODUCTS; ++t) {

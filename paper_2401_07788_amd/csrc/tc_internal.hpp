@@ -176,17 +176,17 @@ struct HeadArgs {
   // head_plan
   uint64_t hq;           // h rounded up to 16
   uint32_t k_logits, k_dx, splits;              // stages of 32 along h and along v; parts of dx's sum
-  uint32_t h_blocks, v_blocks, c_blocks;        // row blocks of 16, up to whole tiles
-  uint64_t wr_plane, xr_plane, wc_plane, xc_plane, pr_plane, pc_plane;         // bytes
+  uint32_t v_blocks, c_blocks;                  // row blocks of 16, up to whole tiles
+  uint64_t wr_plane, xr_plane, pr_plane;        // bytes
   char* info;
   uint32_t* rows;        // [n] tokens that have a target
   float* zt;             // [chunk] logit of the target
-  float* row_lse;        // [chunk]
+  float4* row_info;      // [chunk] lse, weight, target (gradients only)
+  float* rest;           // [chunk] what rounding took from d's entry at the target
   float2* stats;         // [pieces][chunk] maximum and sum of a piece of the vocabulary
-  // operands in blocks (tc_gemm.hpp), rows by summed index
+  // in blocks (tc_gemm.hpp), rows by elements of a row
   char *wr, *xr;         // v by h (nullptr: the call's own w), tokens by h
-  char *wc, *xc;         // h by v, h by tokens
-  char *pr, *pc;         // softmax minus target: tokens by v, v by tokens
+  char* pr;              // d: tokens by v
   char* pt;              // numerators, tokens by v (16-bit types: pr)
   float* dx_part;        // [splits][chunk][hq]
   float* dw_sum;         // [v][hq], or nullptr with one chunk
