@@ -254,12 +254,26 @@ __global__ __launch_bounds__(256) void k_head_pack(const HeadArgs a, uint32_t c0
 }
 
 // ---------------------------------------------------------------- the logits
-// Tile order: 8 token tiles wide, so that the workgroups that run together on
-// a die share rows of both operands.
+// Tile order: 8 tiles of j wide, so that the workgroups that run together on a
+// die share rows of both operands.
 struct Tile { uint32_t i, j; };
 __device__ __forceinline__ Tile tile_of(uint32_t t, uint32_t ni, uint32_t nj) {
   const uint32_t group = t / (8u * ni), rem = t - group * 8u * ni, width = min(8u, nj - group * 8u);
   return {rem / width, group * 8u + rem % width};
+}
+
+// The n-th of a workgroup's tiles out of `total` (false: it has no more).
+// Many tiles: every die takes an eighth of them in a row; few: every round of
+// tiles is dealt out anew (131072 x 8192 x 4096, 64 rounds: 1318 TFLOP/s
+// against 1282; 50304 x 4096 x 768, 12 rounds: 954 against 984).
+__device__ __forceinline__ bool nth_tile(uint32_t n, uint32_t total, uint32_t& t) {
+  if (total >= 32u * gridDim.x) {
+    const uint32_t per = (total + 7u) >> 3, local = n * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    t = (blockIdx.x & 7u) * per + local;
+    return local < per && t < total;
+  }
+  t = n * gridDim.x + die_tile(blockIdx.x, gridDim.x);
+  return t < total;
 }
 
 // pt: softmax numerators relative to their piece's maximum, in the blocks of d
@@ -272,90 +286,92 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
   const Info info = *(const Info*)a.info;
   const uint32_t left = chunk_tokens(a, c0);
   const uint32_t ni = ((uint32_t)a.v + G::TI - 1) / G::TI, nj = (left + G::TJ - 1) / G::TJ;
-  // (only as many tiles as there are tokens for; the grid holds the most there can be)
-  const uint32_t t = die_tile(blockIdx.x, gridDim.x);
-  if (t >= ni * nj) return;
-  const Tile tile = tile_of(t, ni, nj);
-  const uint32_t i0 = tile.i * G::TI, j0 = tile.j * G::TJ;
-  const Blocks B{a.xr, a.c_blocks, a.xr_plane};
-  f32x16 acc[G::WI][G::WJ];
   const uint32_t per = a.k_logits, count = (PL == 2 ? 3 : 1) * per;
-  if constexpr (DIRECT) {
-    const Rows A{(const char*)a.w, a.ldw * 2, (uint32_t)a.v, nullptr};
-    G::template run<1>(A, i0, B, j0, per, 0, count, lds, acc);
-  } else {
-    const Blocks A{a.wr, a.v_blocks, a.wr_plane};
-    G::template run<PL == 2 ? 3 : 1>(A, i0, B, j0, per, 0, count, lds, acc);
-  }
-
-  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h = lane >> 5;
-  const uint32_t iw = i0 + (wave % G::NWI) * (G::WI * 32), jw = j0 + (wave / G::NWI) * (G::WJ * 32) + (lane & 31u);
-  if (iw >= a.v) return;
-  const uint32_t piece = iw / (G::WI * 32);
-  const float scale = Type<T>::PLANES == 2 ? __builtin_ldexpf(1.0f, -plane_exp(info.top_w) - plane_exp(info.top_x)) : 1.0f;
-  // entries past the vocabulary's end, in its last tile
-  if (iw + G::WI * 32 > a.v) {
+  auto work = [&](uint32_t n, typename G::Work& w) {
+    uint32_t t;
+    if (!nth_tile(n, ni * nj, t)) return false;
+    const Tile tile = tile_of(t, ni, nj);
+    w = {tile.i * G::TI, tile.j * G::TJ, 0u, count};
+    return true;
+  };
+  const Blocks B{a.xr, a.c_blocks, a.xr_plane};
+  auto done = [&](uint32_t, const typename G::Work& at, f32x16 (&acc)[G::WI][G::WJ]) {
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h = lane >> 5;
+    const uint32_t iw = at.i0 + (wave % G::NWI) * (G::WI * 32), jw = at.j0 + (wave / G::NWI) * (G::WJ * 32) + (lane & 31u);
+    if (iw >= a.v) return;
+    const uint32_t piece = iw / (G::WI * 32);
+    const float scale = Type<T>::PLANES == 2 ? __builtin_ldexpf(1.0f, -plane_exp(info.top_w) - plane_exp(info.top_x)) : 1.0f;
+    // entries past the vocabulary's end, in its last tile
+    if (iw + G::WI * 32 > a.v) {
 #pragma unroll
-    for (int y = 0; y < G::WJ; ++y)
+      for (int y = 0; y < G::WJ; ++y)
 #pragma unroll
-      for (int x = 0; x < G::WI; ++x)
+        for (int x = 0; x < G::WI; ++x)
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (iw + x * 32 + h * 16 + r >= a.v) acc[x][y][r] = -__builtin_inff();
-  }
-#pragma unroll
-  for (int y = 0; y < G::WJ; ++y) {
-    const uint32_t j = jw + y * 32;
-    float top = -__builtin_inff();
-#pragma unroll
-    for (int x = 0; x < G::WI; ++x)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        if (Type<T>::PLANES == 2) acc[x][y][r] *= scale;
-        top = fmaxf(top, acc[x][y][r]);
-      }
-    top = fmaxf(top, __shfl_xor(top, 32));
-    // the logit of the token's target, where this piece holds it
-    const uint32_t goal = j < left ? (uint32_t)a.target[a.rows[c0 + j]] - iw : ~0u;
-    if (__ballot(goal < G::WI * 32u)) {
-#pragma unroll
-      for (int x = 0; x < G::WI; ++x)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (goal == x * 32 + h * 16 + r) a.zt[j] = acc[x][y][r];
+          for (int r = 0; r < 16; ++r)
+            if (iw + x * 32 + h * 16 + r >= a.v) acc[x][y][r] = -__builtin_inff();
     }
-    // one rounding of top * log2 e is common to the piece: it moves its part of lse by 2^-24 of top
-    float sum = 0.0f;
-    const float shift = -top * LOG2E;
 #pragma unroll
-    for (int x = 0; x < G::WI; ++x) {
+    for (int y = 0; y < G::WJ; ++y) {
+      const uint32_t j = jw + y * 32;
+      float top = -__builtin_inff();
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[x][y][r], LOG2E, shift));
-        acc[x][y][r] = p;
-        sum += p;
+      for (int x = 0; x < G::WI; ++x)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          if (Type<T>::PLANES == 2) acc[x][y][r] *= scale;
+          top = fmaxf(top, acc[x][y][r]);
+        }
+      top = fmaxf(top, __shfl_xor(top, 32));
+      // the logit of the token's target, where this piece holds it
+      const uint32_t goal = j < left ? (uint32_t)a.target[a.rows[c0 + j]] - iw : ~0u;
+      if (__ballot(goal < G::WI * 32u)) {
+#pragma unroll
+        for (int x = 0; x < G::WI; ++x)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (goal == x * 32 + h * 16 + r) a.zt[j] = acc[x][y][r];
       }
-      if (GRAD && j < left) {
-        const uint32_t kb = (iw >> 5) + x;
-        if (kb < a.k_dx) {
-          using N = Numerator<T, WIDE<T, J>>;
-          using R = typename N::R;
-          R v[16];
+      // one rounding of top * log2 e is common to the piece: it moves its part of lse by 2^-24 of top
+      float sum = 0.0f;
+      const float shift = -top * LOG2E;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) v[r] = N::down(acc[x][y][r]);
-          constexpr uint32_t PIECE = 8 * sizeof(R);
-          char* o = a.pt + ((uint64_t)kb * a.c_blocks + (j >> 4)) * (64u * PIECE) + (j & 15u) * 4u * PIECE;
-          if constexpr (WIDE<T, J>) {
-            __builtin_memcpy(o + h * 2 * PIECE, v, 2 * PIECE);
-          } else {
-            __builtin_memcpy(o + ((2u * h) ^ turn(j)) * PIECE, v, PIECE);
-            __builtin_memcpy(o + ((2u * h + 1u) ^ turn(j)) * PIECE, v + 8, PIECE);
+      for (int x = 0; x < G::WI; ++x) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[x][y][r], LOG2E, shift));
+          acc[x][y][r] = p;
+          sum += p;
+        }
+        if (GRAD && j < left) {
+          const uint32_t kb = (iw >> 5) + x;
+          if (kb < a.k_dx) {
+            using N = Numerator<T, WIDE<T, J>>;
+            using R = typename N::R;
+            R v[16];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) v[r] = N::down(acc[x][y][r]);
+            constexpr uint32_t PIECE = 8 * sizeof(R);
+            char* o = a.pt + ((uint64_t)kb * a.c_blocks + (j >> 4)) * (64u * PIECE) + (j & 15u) * 4u * PIECE;
+            if constexpr (WIDE<T, J>) {
+              __builtin_memcpy(o + h * 2 * PIECE, v, 2 * PIECE);
+            } else {
+              __builtin_memcpy(o + ((2u * h) ^ turn(j)) * PIECE, v, PIECE);
+              __builtin_memcpy(o + ((2u * h + 1u) ^ turn(j)) * PIECE, v + 8, PIECE);
+            }
           }
         }
       }
+      sum += __shfl_xor(sum, 32);
+      if (h == 0 && j < left) a.stats[(uint64_t)piece * a.chunk + j] = make_float2(top, sum);
     }
-    sum += __shfl_xor(sum, 32);
-    if (h == 0 && j < left) a.stats[(uint64_t)piece * a.chunk + j] = make_float2(top, sum);
+  };
+  if constexpr (DIRECT) {
+    const Rows A{(const char*)a.w, a.ldw * 2, (uint32_t)a.v, nullptr};
+    G::template stream<1>(A, B, per, lds, work, done);
+  } else {
+    const Blocks A{a.wr, a.v_blocks, a.wr_plane};
+    G::template stream<PL == 2 ? 3 : 1>(A, B, per, lds, work, done);
   }
 }
 
@@ -459,31 +475,38 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
   extern __shared__ __attribute__((aligned(128))) char lds[];
   const uint32_t left = chunk_tokens(a, c0);
   const uint32_t ni = (a.h + G::TI - 1) / G::TI, nj = (left + G::TJ - 1) / G::TJ;
-  const uint32_t t = die_tile(blockIdx.x, gridDim.x);
-  if (t >= ni * nj * a.splits) return;
-  // a part's tiles together: they share its rows of w and of the softmax
-  const uint32_t split = t / (ni * nj);
-  const Tile tile = tile_of(t - split * ni * nj, ni, nj);
-  const uint32_t i0 = tile.i * G::TI, j0 = tile.j * G::TJ;
   const uint32_t all = (Type<T>::PLANES == 2 ? 3 : 1) * a.k_dx;
-  const uint32_t s0 = (uint32_t)((uint64_t)all * split / a.splits), s1 = (uint32_t)((uint64_t)all * (split + 1) / a.splits);
+  auto work = [&](uint32_t n, typename G::Work& w) {
+    uint32_t t;
+    if (!nth_tile(n, ni * nj * a.splits, t)) return false;
+    // a part's tiles together: they share its rows of w and of d
+    const uint32_t split = t / (ni * nj);
+    const Tile tile = tile_of(t - split * ni * nj, ni, nj);
+    const uint32_t s0 = (uint32_t)((uint64_t)all * split / a.splits), s1 = (uint32_t)((uint64_t)all * (split + 1) / a.splits);
+    w = {tile.i * G::TI, tile.j * G::TJ, s0, s1 - s0};
+    return true;
+  };
+  auto done = [&](uint32_t, const typename G::Work& at, f32x16 (&acc)[G::WI][G::WJ]) {
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h = lane >> 5;
+    const uint32_t iw = at.i0 + (wave % G::NWI) * (G::WI * 32) + h * 16, jw = at.j0 + (wave / G::NWI) * (G::WJ * 32) + (lane & 31u);
+    // (the part that starts at s0: the first that does not end before it)
+    uint32_t split = (uint32_t)((uint64_t)at.s0 * a.splits / all);
+    if ((uint64_t)all * split / a.splits != at.s0) ++split;
+#pragma unroll
+    for (int y = 0; y < G::WJ; ++y)
+#pragma unroll
+      for (int x = 0; x < G::WI; ++x) {
+        const uint32_t i = iw + x * 32, j = jw + y * 32;
+        if (i >= a.hq || j >= left) continue;
+        float4* o = reinterpret_cast<float4*>(a.dx_part + ((uint64_t)split * a.chunk + j) * a.hq + i);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          o[q] = make_float4(acc[x][y][q * 4], acc[x][y][q * 4 + 1], acc[x][y][q * 4 + 2], acc[x][y][q * 4 + 3]);
+      }
+  };
   const BlocksT A{a.wr, a.v_blocks, a.wr_plane};
   const Blocks B{a.pr, a.c_blocks, a.pr_plane};
-  f32x16 acc[G::WI][G::WJ];
-  G::template run<Type<T>::PLANES == 2 ? 3 : 1>(A, i0, B, j0, a.k_dx, s0, s1 - s0, lds, acc);
-  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h = lane >> 5;
-  const uint32_t iw = i0 + (wave % G::NWI) * (G::WI * 32) + h * 16, jw = j0 + (wave / G::NWI) * (G::WJ * 32) + (lane & 31u);
-#pragma unroll
-  for (int y = 0; y < G::WJ; ++y)
-#pragma unroll
-    for (int x = 0; x < G::WI; ++x) {
-      const uint32_t i = iw + x * 32, j = jw + y * 32;
-      if (i >= a.hq || j >= left) continue;
-      float4* o = reinterpret_cast<float4*>(a.dx_part + ((uint64_t)split * a.chunk + j) * a.hq + i);
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        o[q] = make_float4(acc[x][y][q * 4], acc[x][y][q * 4 + 1], acc[x][y][q * 4 + 2], acc[x][y][q * 4 + 3]);
-    }
+  G::template stream<Type<T>::PLANES == 2 ? 3 : 1>(A, B, a.k_dx, lds, work, done);
 }
 
 // dx of the list's places c0 + blockIdx.x: the parts' sum, and what the target's entry of d lost when it was rounded:
@@ -513,61 +536,151 @@ __global__ __launch_bounds__(256) void k_head_dx_sum(const HeadArgs a, uint32_t 
   }
 }
 
-// dw: a tile of vocabulary entries by hidden positions, summed over the
-// chunk's tokens.  One chunk: rounded to its dtype here.  More: binary32 sums
-// from chunk to chunk, rounded by k_head_dw_round after the last.
+// dw: tiles of vocabulary entries by hidden positions, summed over the chunk's
+// tokens.  Whole rounds of tiles (one for every workgroup) are summed by one
+// workgroup each; those of the last, partial round are split along the
+// tokens, so that it takes a part of a round, and joined by k_head_dw_tail.
+// One chunk: rounded to its dtype here.  More: binary32 sums from chunk to
+// chunk, rounded by k_head_dw_round after the last.
 template <typename T>
-__global__ __launch_bounds__((Cfg<typename Type<T>::V8, 256>::NT), 2) void k_head_dw(const HeadArgs a, uint32_t c0) {
+struct DwPlan {
   using G = Cfg<typename Type<T>::V8, 256>;
+  uint32_t ni, nj, whole, rest, all, parts;
+  __device__ __forceinline__ DwPlan(const HeadArgs& a, uint32_t left) {
+    ni = (a.h + G::TI - 1) / G::TI;
+    nj = ((uint32_t)a.v + G::TJ - 1) / G::TJ;
+    whole = ni * nj / a.dw_grid * a.dw_grid;
+    rest = ni * nj - whole;
+    all = (Type<T>::PLANES == 2 ? 3 : 1) * ((left + KSTAGE - 1) / KSTAGE);
+    parts = min(a.dw_parts, all);       // (each has a stage at least)
+  }
+  __device__ __forceinline__ Tile tile(uint32_t t) const {
+    const Tile x = tile_of(t, nj, ni);
+    return {x.j, x.i};
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void dw_store(const HeadArgs& a, uint32_t c0, float f, uint32_t i, uint32_t j, const float (&v)[16]) {
   using R = typename Elem<T>::raw;
-  extern __shared__ __attribute__((aligned(128))) char lds[];
+  if (i >= a.h || j >= a.v) return;
+  if (a.dw_sum) {
+    float* o = a.dw_sum + (uint64_t)j * a.hq + i;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      float4 s = make_float4(v[q * 4] * f, v[q * 4 + 1] * f, v[q * 4 + 2] * f, v[q * 4 + 3] * f);
+      if (c0 > 0) {
+        const float4 old = reinterpret_cast<const float4*>(o)[q];
+        s = make_float4(s.x + old.x, s.y + old.y, s.z + old.z, s.w + old.w);
+      }
+      reinterpret_cast<float4*>(o)[q] = s;
+    }
+  } else {
+    R w[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) w[r] = Elem<T>::down(v[r] * f);
+    R* o = (R*)a.dw + (uint64_t)j * a.h + i;
+    if (i + 16 <= a.h) {
+      store_run<R, 16>(o, w);
+    } else {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (i + r < a.h) o[r] = w[r];
+    }
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ float dw_factor(const HeadArgs& a) {
   const Info info = *(const Info*)a.info;
-  const uint32_t left = chunk_tokens(a, c0);
-  if (c0 > 0 && left == 0) return;
-  const uint32_t ni = (a.h + G::TI - 1) / G::TI, nj = ((uint32_t)a.v + G::TJ - 1) / G::TJ;
-  const uint32_t t = die_tile(blockIdx.x, gridDim.x);
-  if (t >= ni * nj) return;
-  const uint32_t i0 = t % ni * G::TI, j0 = t / ni * G::TJ;
-  const uint32_t per = (left + KSTAGE - 1) / KSTAGE;
-  const BlocksT A{a.xr, a.c_blocks, a.xr_plane}, B{a.pr, a.c_blocks, a.pr_plane};
-  f32x16 acc[G::WI][G::WJ];
-  G::template run<Type<T>::PLANES == 2 ? 3 : 1>(A, i0, B, j0, per, 0, (Type<T>::PLANES == 2 ? 3 : 1) * per, lds, acc);
   float f = 1.0f / P_SCALE<T>;
   if (!std::is_same_v<T, bf16_t>) f *= __uint_as_float(info.top_g);
   if (Type<T>::PLANES == 2) f = __builtin_ldexpf(f, -plane_exp(info.top_x));
+  return f;
+}
+
+template <typename T>
+__global__ __launch_bounds__((Cfg<typename Type<T>::V8, 256>::NT), 2) void k_head_dw(const HeadArgs a, uint32_t c0) {
+  using G = Cfg<typename Type<T>::V8, 256>;
+  extern __shared__ __attribute__((aligned(128))) char lds[];
+  const uint32_t left = chunk_tokens(a, c0);
+  if (c0 > 0 && left == 0) return;
+  const DwPlan<T> plan(a, left);
+  const float f = dw_factor<T>(a);
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h = lane >> 5;
-  const uint32_t iw = i0 + (wave % G::NWI) * (G::WI * 32) + h * 16, jw = j0 + (wave / G::NWI) * (G::WJ * 32) + (lane & 31u);
+  const uint32_t mine = die_tile(blockIdx.x, gridDim.x);
+  auto done = [&](uint32_t n, const typename G::Work& at, f32x16 (&acc)[G::WI][G::WJ]) {
+    const uint32_t iw = at.i0 + (wave % G::NWI) * (G::WI * 32) + h * 16, jw = at.j0 + (wave / G::NWI) * (G::WJ * 32) + (lane & 31u);
+    // (of no stages: the zeros of a chunk without tokens)
+    const bool part = at.count != 0 && n * gridDim.x >= plan.whole;
 #pragma unroll
-  for (int y = 0; y < G::WJ; ++y)
+    for (int y = 0; y < G::WJ; ++y)
 #pragma unroll
-    for (int x = 0; x < G::WI; ++x) {
-      const uint32_t i = iw + x * 32, j = jw + y * 32;
-      if (i >= a.h || j >= a.v) continue;
-      if (a.dw_sum) {
-        float* o = a.dw_sum + (uint64_t)j * a.hq + i;
+      for (int x = 0; x < G::WI; ++x) {
+        float v[16];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          float4 s = make_float4(acc[x][y][q * 4] * f, acc[x][y][q * 4 + 1] * f, acc[x][y][q * 4 + 2] * f, acc[x][y][q * 4 + 3] * f);
-          if (c0 > 0) {
-            const float4 old = reinterpret_cast<const float4*>(o)[q];
-            s = make_float4(s.x + old.x, s.y + old.y, s.z + old.z, s.w + old.w);
-          }
-          reinterpret_cast<float4*>(o)[q] = s;
-        }
-      } else {
-        R v[16];
+        for (int r = 0; r < 16; ++r) v[r] = acc[x][y][r];
+        if (part) {
+          // as the lanes hold them: k_head_dw_tail reads them the same way
+          float4* o = reinterpret_cast<float4*>(a.dw_part + ((uint64_t)mine * (G::WI * G::WJ) + y * G::WI + x) * (G::NT * 16)) + threadIdx.x * 4;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) v[r] = Elem<T>::down(acc[x][y][r] * f);
-        R* o = (R*)a.dw + (uint64_t)j * a.h + i;
-        if (i + 16 <= a.h) {
-          store_run<R, 16>(o, v);
+          for (int q = 0; q < 4; ++q) o[q] = make_float4(v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]);
         } else {
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (i + r < a.h) o[r] = v[r];
+          dw_store<T>(a, c0, f, iw + x * 32, jw + y * 32, v);
         }
       }
+  };
+  if (left == 0) {
+    // nothing to sum: zeros
+    f32x16 zero[G::WI][G::WJ] = {};
+    for (uint32_t t = mine; t < plan.ni * plan.nj; t += gridDim.x) {
+      const Tile x = plan.tile(t);
+      done(0, {x.i * G::TI, x.j * G::TJ, 0u, 0u}, zero);
     }
+    return;
+  }
+  auto work = [&](uint32_t n, typename G::Work& w) {
+    uint32_t t = n * gridDim.x + mine, s0 = 0, s1 = plan.all;
+    if (n * gridDim.x >= plan.whole) {
+      if (n * gridDim.x > plan.whole || mine >= plan.rest * plan.parts) return false;
+      const uint32_t split = mine / plan.rest;
+      t = plan.whole + mine - split * plan.rest;
+      s0 = plan.all * split / plan.parts;
+      s1 = plan.all * (split + 1) / plan.parts;
+    }
+    const Tile x = plan.tile(t);
+    w = {x.i * G::TI, x.j * G::TJ, s0, s1 - s0};
+    return true;
+  };
+  const BlocksT A{a.xr, a.c_blocks, a.xr_plane}, B{a.pr, a.c_blocks, a.pr_plane};
+  G::template stream<Type<T>::PLANES == 2 ? 3 : 1>(A, B, (left + KSTAGE - 1) / KSTAGE, lds, work, done);
+}
+
+// one fragment row of a tile of the last round per workgroup
+template <typename T>
+__global__ __launch_bounds__((Cfg<typename Type<T>::V8, 256>::NT)) void k_head_dw_tail(const HeadArgs a, uint32_t c0) {
+  using G = Cfg<typename Type<T>::V8, 256>;
+  const uint32_t left = chunk_tokens(a, c0);
+  if (left == 0) return;
+  const DwPlan<T> plan(a, left);
+  const uint32_t tile = blockIdx.x / (G::WI * G::WJ), xy = blockIdx.x % (G::WI * G::WJ), x = xy % G::WI, y = xy / G::WI;
+  float v[16] = {};
+  for (uint32_t p = 0; p < plan.parts; ++p) {
+    const float4* s = reinterpret_cast<const float4*>(a.dw_part + ((uint64_t)(p * plan.rest + tile) * (G::WI * G::WJ) + xy) * (G::NT * 16)) + threadIdx.x * 4;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float4 u = s[q];
+      v[q * 4] += u.x;
+      v[q * 4 + 1] += u.y;
+      v[q * 4 + 2] += u.z;
+      v[q * 4 + 3] += u.w;
+    }
+  }
+  const Tile at = plan.tile(plan.whole + tile);
+  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h = lane >> 5;
+  const uint32_t i = at.i * G::TI + (wave % G::NWI) * (G::WI * 32) + h * 16 + x * 32;
+  const uint32_t j = at.j * G::TJ + (wave / G::NWI) * (G::WJ * 32) + (lane & 31u) + y * 32;
+  dw_store<T>(a, c0, dw_factor<T>(a), i, j, v);
 }
 
 template <typename T>
@@ -594,8 +707,16 @@ hipError_t launch_lds(uint32_t grid, uint32_t nt, uint32_t lds, hipStream_t st, 
     HEAD_TRY(hipFuncSetAttribute((const void*)K, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
     if (dev < 64) asked.fetch_or(1ull << dev, std::memory_order_relaxed);
   }
-  hipLaunchKernelGGL(K, dim3((grid + 7) / 8 * 8), dim3(nt), lds, st, a, c0);
+  hipLaunchKernelGGL(K, dim3(grid), dim3(nt), lds, st, a, c0);
   return hipGetLastError();
+}
+
+// workgroups of a product's kernel: as many as run at once, or as there are
+// tiles, in eights
+template <typename G>
+uint32_t grid_of(uint64_t tiles) {
+  const uint64_t room = (uint64_t)(device_cus() * G::PER_CU + 7) / 8 * 8;
+  return (uint32_t)std::min<uint64_t>(room, (tiles + 7) / 8 * 8);
 }
 
 template <typename T, int J, bool GRAD>
@@ -610,12 +731,12 @@ hipError_t chunk_of(HeadArgs& a, uint32_t c0, uint32_t rows, hipStream_t st) {
   HEAD_TRY(hipGetLastError());
   if constexpr (!GRAD && Type<T>::PLANES == 1) {
     if (!a.wr) {
-      HEAD_TRY((launch_lds<k_head_logits<T, J, false, true>>(ni * nj, G::NT, G::LDS, st, a, c0)));
+      HEAD_TRY((launch_lds<k_head_logits<T, J, false, true>>(grid_of<G>(ni * nj), G::NT, G::LDS, st, a, c0)));
     } else {
-      HEAD_TRY((launch_lds<k_head_logits<T, J, false, false>>(ni * nj, G::NT, G::LDS, st, a, c0)));
+      HEAD_TRY((launch_lds<k_head_logits<T, J, false, false>>(grid_of<G>(ni * nj), G::NT, G::LDS, st, a, c0)));
     }
   } else {
-    HEAD_TRY((launch_lds<k_head_logits<T, J, GRAD, false>>(ni * nj, G::NT, G::LDS, st, a, c0)));
+    HEAD_TRY((launch_lds<k_head_logits<T, J, GRAD, false>>(grid_of<G>(ni * nj), G::NT, G::LDS, st, a, c0)));
   }
   hipLaunchKernelGGL(k_head_loss, dim3((rows + SR - 1) / SR), dim3(SNT), 0, st, a, c0, pieces,
                      !std::is_same_v<T, bf16_t>);
@@ -625,14 +746,18 @@ hipError_t chunk_of(HeadArgs& a, uint32_t c0, uint32_t rows, hipStream_t st) {
                        PIECE == 128 ? 7u : 6u);
     HEAD_TRY(hipGetLastError());
     const uint32_t nh = (a.h + G::TI - 1) / G::TI;
-    HEAD_TRY((launch_lds<k_head_dx<T, J>>(nh * nj * a.splits, G::NT, G::LDS, st, a, c0)));
+    HEAD_TRY((launch_lds<k_head_dx<T, J>>(grid_of<G>((uint64_t)nh * nj * a.splits), G::NT, G::LDS, st, a, c0)));
     if (a.n > 0) {
       hipLaunchKernelGGL((k_head_dx_sum<T>), dim3(rows), dim3(256), 0, st, a, c0);
       HEAD_TRY(hipGetLastError());
     }
     using W = Cfg<typename Type<T>::V8, 256>;
-    const uint32_t tiles = ((a.h + W::TI - 1) / W::TI) * (((uint32_t)a.v + W::TJ - 1) / W::TJ);
-    HEAD_TRY((launch_lds<k_head_dw<T>>(tiles, W::NT, W::LDS, st, a, c0)));
+    HEAD_TRY((launch_lds<k_head_dw<T>>(a.dw_grid, W::NT, W::LDS, st, a, c0)));
+    if (a.dw_parts) {
+      const uint32_t tiles = ((a.h + W::TI - 1) / W::TI) * (((uint32_t)a.v + W::TJ - 1) / W::TJ);
+      hipLaunchKernelGGL((k_head_dw_tail<T>), dim3(tiles % a.dw_grid * (W::WI * W::WJ)), dim3(W::NT), 0, st, a, c0);
+      HEAD_TRY(hipGetLastError());
+    }
   }
   return hipSuccess;
 }
@@ -677,7 +802,7 @@ uint64_t head_plan(HeadArgs& a, int dt, bool grad, char* base) {
   // replaced in place)
   const uint64_t per_row = grad ? (uint64_t)a.k_dx * KSTAGE * (planes == 2 ? 8 : 2) : (a.v + 63) / 64 * 8;
   if (a.chunk == 0) a.chunk = HEAD_CHUNK_BYTES / per_row;
-  a.chunk = std::min<uint64_t>(std::max<uint64_t>(a.chunk, 128), (a.n + 64) / 64 * 64);
+  a.chunk = std::min<uint64_t>(std::max<uint64_t>(a.chunk, 128), std::max<uint64_t>(a.n, 1));
   a.chunk = (a.chunk + 63) / 64 * 64;
   a.c_blocks = blocks(a.chunk);
   const bool one = a.chunk >= a.n;
@@ -707,12 +832,27 @@ uint64_t head_plan(HeadArgs& a, int dt, bool grad, char* base) {
     a.pt = planes == 2 || a.chunk <= 64 ? take(a.pr_plane * 2) : a.pr;
     a.row_info = (float4*)take(a.chunk * 16);
     a.rest = (float*)take(a.chunk * 4);
-    // as many parts of the vocabulary as give every compute unit its
-    // workgroups, none below 16 stages
+    // dx: parts of the vocabulary, as many as cost least: rounds of tiles
+    // (about half a microsecond a stage) and the parts' sums written and read
     const uint64_t tj = tile_tokens(a.chunk), tiles = (a.h + 255) / 256 * ((a.chunk + tj - 1) / tj);
     const uint64_t stages = (planes == 2 ? 3 : 1) * (uint64_t)a.k_dx, room = (tj == 256 ? 1 : 2) * (uint64_t)device_cus();
-    a.splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(room / std::max<uint64_t>(tiles, 1), stages / 16));
+    double best = 0.0;
+    a.splits = 0;
+    for (uint64_t s = 1; s <= std::max<uint64_t>(1, std::min<uint64_t>(stages / 16, room)); ++s) {
+      const double cost = (double)((tiles * s + room - 1) / room) * ((double)stages / (double)s + 8.0) * 0.5e-6 +
+                          (double)(s * a.chunk * a.hq) * 8.0 / 5e12;
+      if (a.splits == 0 || cost < best) {
+        best = cost;
+        a.splits = (uint32_t)s;
+      }
+    }
     a.dx_part = (float*)take(a.splits * a.chunk * a.hq * 4);
+    // dw: the tiles past the last whole round in as many parts as fill one
+    const uint64_t wt = (a.h + 255) / 256 * ((a.v + 255) / 256), cus = (uint64_t)(device_cus() + 7) / 8 * 8;
+    a.dw_grid = (uint32_t)std::min<uint64_t>(cus, (wt + 7) / 8 * 8);
+    const uint64_t rest = wt % a.dw_grid;
+    a.dw_parts = rest ? (uint32_t)std::min<uint64_t>(a.dw_grid / rest, 16) : 0;
+    a.dw_part = (float*)take(rest * a.dw_parts * 256 * 256 * 4);
     a.dw_sum = one ? nullptr : (float*)take(a.v * a.hq * 4);
   }
   return at;

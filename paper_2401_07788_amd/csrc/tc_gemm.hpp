@@ -101,14 +101,15 @@ template <uint32_t L> struct Loader<Blocks, L> {
     else if (t == 2) load16<2048>(g, to);
     else load16<3072>(g, to);
   }
-  __device__ __forceinline__ void next(bool more) { at += more ? stage : 0; }
+  __device__ __forceinline__ void next() { at += stage; }
+  __device__ __forceinline__ void stay() { at -= stage; stage = 0; }
   // from the end of one walk over k to the start of another, in the same plane (0) or the other (+1, -1)
   __device__ __forceinline__ void again(uint32_t per, int to) { at += (int64_t)plane * to - (int64_t)(stage * per); }
 };
 template <uint32_t L> struct Loader<BlocksT, L> {
   const char* at;
   uint64_t plane;
-  uint32_t pitch, lane16;
+  uint32_t pitch, lane16, stage = 2048;
   __device__ __forceinline__ Loader(const BlocksT& o, uint32_t row0, uint32_t wave, uint32_t k) {
     // load b of the stage is block (b & 1) along the sum, 32 rows from row0 + 32 (b >> 1) on
     const uint32_t b = wave * L;
@@ -124,12 +125,13 @@ template <uint32_t L> struct Loader<BlocksT, L> {
     if (t & 1) load16<1024>(g, to + (t & 2) * 1024u);
     else load16<0>(g, to + (t & 2) * 1024u);
   }
-  __device__ __forceinline__ void next(bool more) { at += more ? 2048 : 0; }
+  __device__ __forceinline__ void next() { at += stage; }
+  __device__ __forceinline__ void stay() { at -= stage; stage = 0; }
   __device__ __forceinline__ void again(uint32_t per, int to) { at += (int64_t)plane * to - (int64_t)(2048u * per); }
 };
 template <uint32_t L> struct Loader<Rows, L> {
   const char* at;
-  uint32_t off[L];
+  uint32_t off[L], stage = ROW_BYTES;
   __device__ __forceinline__ Loader(const Rows& o, uint32_t row0, uint32_t wave, uint32_t k) {
     const uint32_t lane = threadIdx.x & 63u;
     at = (o.map ? o.p : o.p + (uint64_t)row0 * o.ld) + (uint64_t)k * ROW_BYTES;
@@ -143,7 +145,8 @@ template <uint32_t L> struct Loader<Rows, L> {
     asm volatile("" : "+v"(off[t]));
     load16<0>(at + off[t], to + t * 1024u);
   }
-  __device__ __forceinline__ void next(bool more) { at += more ? ROW_BYTES : 0; }
+  __device__ __forceinline__ void next() { at += stage; }
+  __device__ __forceinline__ void stay() { at -= stage; stage = 0; }
   __device__ __forceinline__ void again(uint32_t, int) {}
 };
 
@@ -196,40 +199,58 @@ struct Gemm {
     }
   };
 
-  // stages [s0, s0 + count) of the walk over the pairs of planes (one, or
-  // three: high high, high low, low high), `per` stages each
-  template <int PAIRS, typename OA, typename OB>
-  static __device__ __forceinline__ void run(const OA& A, uint32_t i0, const OB& B, uint32_t j0, uint32_t per, uint32_t s0,
-                                             uint32_t count, char* lds, f32x16 (&acc)[WI][WJ]) {
-    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-#pragma unroll
-    for (int x = 0; x < WI; ++x)
-#pragma unroll
-      for (int y = 0; y < WJ; ++y) acc[x][y] = f32x16{};
-    if (count == 0) return;
+  // A piece of work: stages [s0, s0 + count) of the tile at (i0, j0), count > 0.
+  // The walk along k goes over the pairs of planes (one, or three: high high,
+  // high low, low high), `per` stages each.
+  struct Work {
+    uint32_t i0, j0, s0, count;
+  };
 
-    uint32_t pair = PAIRS > 1 ? s0 / per : 0, k = s0 - pair * per, left = count;
-    Loader<OA, LA> ga(A, i0, wave, k);
-    Loader<OB, LB> gb(B, j0, wave, k);
-    if constexpr (PAIRS > 1) {
-      if (pair == 2) ga.again(0, 1);
-      if (pair == 1) gb.again(0, 1);
-    }
-    // to the next stage; past the last one that is loaded again, into a slot
-    // that nobody reads, so that every stage has the same loads out
-    auto advance = [&] {
-      const bool more = left > 1;
-      left -= more;
-      ga.next(more);
-      gb.next(more);
+  // The workgroup's pieces one after the other: work(n, w) gives the n-th or
+  // returns false, done(n, w, acc) takes its sums.  The stages of all of them
+  // are one stream: while the last ones of a piece are multiplied, the first
+  // ones of the next are loaded, and they land while done() runs (which
+  // therefore has no LDS).
+  template <int PAIRS, typename OA, typename OB, typename WorkOf, typename Done>
+  static __device__ __forceinline__ void stream(const OA& A, const OB& B, uint32_t per, char* lds, WorkOf work, Done done) {
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Work in;                                             // of the loads
+    uint32_t n_in = 0;
+    if (!work(0u, in)) return;
+    Work out = in;                                       // of the products
+    uint32_t pair, left, rest;         // stages to load until the next turn, and of the piece after that
+    Loader<OA, LA> ga(A, 0, wave, 0);
+    Loader<OB, LB> gb(B, 0, wave, 0);
+    auto begin = [&] {
+      pair = PAIRS > 1 ? in.s0 / per : 0;
+      const uint32_t k = in.s0 - pair * per;
+      left = PAIRS > 1 ? min(in.count, per - k) : in.count;
+      rest = in.count - left;
+      ga = Loader<OA, LA>(A, in.i0, wave, k);
+      gb = Loader<OB, LB>(B, in.j0, wave, k);
       if constexpr (PAIRS > 1) {
-        k += more;
-        if (k == per && more) {
-          k = 0;
-          ++pair;
-          ga.again(per, pair == 2 ? 1 : 0);
-          gb.again(per, pair == 1 ? 1 : -1);
-        }
+        if (pair == 2) ga.again(0, 1);
+        if (pair == 1) gb.again(0, 1);
+      }
+    };
+    begin();
+    // where the walk turns: to the next pair of planes, the next piece, or,
+    // after the very last stage, to that stage again and again (into slots
+    // that nobody reads, so that every stage has the same loads out)
+    auto turn_over = [&] {
+      if (PAIRS > 1 && rest > 0) {
+        left = min(rest, per);
+        rest -= left;
+        ++pair;
+        ga.again(per, pair == 2 ? 1 : 0);
+        gb.again(per, pair == 1 ? 1 : -1);
+      } else if (work(++n_in, in)) {
+        begin();
+      } else {
+        --n_in;
+        left = ~0u;
+        ga.stay();
+        gb.stay();
       }
     };
     char* const la = lds + wave * LA * 1024u;
@@ -254,12 +275,15 @@ struct Gemm {
     for (uint32_t s = 0; s < NS - 1; ++s) {
 #pragma unroll
       for (uint32_t t = 0; t < LOADS; ++t) load(s * SLOT, t);
-      advance();
+      ga.next();
+      gb.next();
+      if (--left == 0) turn_over();
     }
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((NS - 2) * LOADS) : "memory");
 #pragma unroll
     for (uint32_t n = 0; n < READS; ++n) read(lds, f0, n);
     uint32_t to = (NS - 1) * SLOT, from = SLOT;       // slots of the stage to load and to read
+    f32x16 acc[WI][WJ];
     auto step = [&](const Frags& now, Frags& then) {
       // the stage to read has landed for every wavefront, and every wavefront
       // has the stage before the present one in registers or behind it
@@ -267,8 +291,8 @@ struct Gemm {
       __builtin_amdgcn_sched_barrier(0);
       const char* s = lds + from;
       // a read beside every product until all are out, and the loads spread
-      // over the stage: a wavefront issues in order, and 8 wavefronts' loads at
-      // once would hold up the products behind them
+      // over the stage: a wavefront issues in order, and what it issues at once
+      // holds up the products behind it
 #pragma unroll
       for (uint32_t m = 0; m < PRODUCTS; ++m) {
         const uint32_t q = m / (WI * WJ), x = m / WJ % WI, y = m % WJ;
@@ -287,22 +311,45 @@ struct Gemm {
       }
 #pragma unroll
       for (uint32_t n = PRODUCTS; n < READS; ++n) read(s, then, n);
-      advance();
+      ga.next();
+      gb.next();
       to = to == (NS - 1) * SLOT ? 0 : to + SLOT;
       from = from == (NS - 1) * SLOT ? 0 : from + SLOT;
       __builtin_amdgcn_sched_barrier(0);
     };
-    for (uint32_t s = 0; s < count; s += 2) {
-      step(f0, f1);
-      if (s + 1 < count) step(f1, f0);
+    for (uint32_t n_out = 0;;) {
+#pragma unroll
+      for (int x = 0; x < WI; ++x)
+#pragma unroll
+        for (int y = 0; y < WJ; ++y) acc[x][y] = f32x16{};
+      for (uint32_t s = 0; s < out.count;) {
+        // (no stage asks whether the walk turns there)
+        const uint32_t run = min(out.count - s, left);
+        for (uint32_t r = 0; r < run; r += 2) {
+          step(f0, f1);
+          if (r + 1 < run) step(f1, f0);
+        }
+        if (run & 1) f0 = f1;
+        s += run;
+        left -= run;
+        if (left == 0) turn_over();
+      }
+      done(n_out, out, acc);
+      if (!work(++n_out, out)) break;
+      // the next piece's first stage again: held across done(), its fragments
+      // would take the registers that done() needs
+      const char* s = lds + (from == 0 ? (NS - 1) * SLOT : from - SLOT);
+#pragma unroll
+      for (uint32_t n = 0; n < READS; ++n) read(s, f0, n);
     }
-    // loads that nobody reads must not land in what the caller puts there
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    // the last loads land before the LDS is given up
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   }
 };
 
 // Workgroups go round the 8 dies in turn; tiles that share operands should
-// share a die's cache: die d takes the d-th run of consecutive tiles.
+// share a die's cache: of `blocks` tiles, a multiple of 8, die d takes the
+// d-th run of consecutive ones.
 __device__ __forceinline__ uint32_t die_tile(uint32_t block, uint32_t blocks) { return (block & 7u) * (blocks >> 3) + (block >> 3); }
 
 }  // namespace tc

@@ -190,6 +190,8 @@ struct HeadArgs {
   char* pt;              // numerators, tokens by v (16-bit types: pr)
   float* dx_part;        // [splits][chunk][hq]
   float* dw_sum;         // [v][hq], or nullptr with one chunk
+  uint32_t dw_grid, dw_parts;   // workgroups of dw's product; parts of its last round's tiles
+  float* dw_part;        // [tiles of the last round][dw_parts][256 * 256]
 };
 // bytes that the per-token buffers of a chunk may take unless the caller chooses
 constexpr uint64_t HEAD_CHUNK_BYTES = 4ull << 30;
