@@ -398,7 +398,8 @@ tc_status tc_grad_norm(const tc_tensor* list, uint64_t n_list, int g_dt, float m
                        size_t ws_bytes, void* stream);
 
 /* AdamW's settings and moments.
- *   lr, beta1, beta2, eps, weight_decay   0 <= beta < 1, eps >= 0
+ *   lr, beta1, beta2, eps, weight_decay   0 <= beta < 1, eps >= 0 (8 bits:
+ *          >= 1e-15)
  *   t      this step's number, from 1 on (bias correction)
  *   bits   32: m and v are binary32 [positions]
  *          8: m and v are codes (a byte per position) and em, ev the exponents

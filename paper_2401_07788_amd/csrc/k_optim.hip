@@ -52,12 +52,13 @@ __device__ __forceinline__ void put(void* base, uint64_t i, const R (&in)[N]) {
   *reinterpret_cast<V*>(static_cast<R*>(base) + i) = v;
 }
 
-// `left` of OV elements exist (left <= 0: none); the others read as zero
-template <typename T>
+// `left` of OV elements exist (left <= 0: none); the others read as zero.
+// FULL: all of them do, for every lane.
+template <typename T, bool FULL>
 __device__ __forceinline__ void load_up(const void* base, uint64_t i, int64_t left, float (&out)[OV]) {
   using R = typename Elem<T>::raw;
   R r[OV];
-  if (left >= OV) {
+  if (FULL || left >= OV) {
     get<R, OV>(base, i, r);
 #pragma unroll
     for (int k = 0; k < OV; ++k) out[k] = Elem<T>::up(r[k]);
@@ -66,13 +67,13 @@ __device__ __forceinline__ void load_up(const void* base, uint64_t i, int64_t le
     for (int k = 0; k < OV; ++k) out[k] = k < left ? Elem<T>::up(static_cast<const R*>(base)[i + k]) : 0.0f;
   }
 }
-template <typename T>
+template <typename T, bool FULL>
 __device__ __forceinline__ void store_down(void* base, uint64_t i, int64_t left, const float (&in)[OV]) {
   using R = typename Elem<T>::raw;
   R r[OV];
 #pragma unroll
   for (int k = 0; k < OV; ++k) r[k] = Elem<T>::down(in[k]);
-  if (left >= OV) {
+  if (FULL || left >= OV) {
     put<R, OV>(base, i, r);
   } else {
 #pragma unroll
@@ -141,6 +142,90 @@ __device__ __forceinline__ uint32_t half_wave_max(uint32_t x) {
 }  // namespace
 
 // ------------------------------------------------------------------- AdamW
+// p after the step.  Next to 28 or 22 bytes an element the exact division and
+// square root cost nothing; next to 10 they would be the bound, and the
+// hardware's (each within an ulp, of a step that is far smaller than p) are
+// used.  Those take a v below 2^-126 for 0, which eps covers.
+template <bool EIGHT>
+__device__ __forceinline__ float adamw_p(const AdamwArgs& a, float p, float m, float v) {
+  if constexpr (EIGHT)
+    return p * a.decay - m * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v * a.r2) + a.eps) * a.rate;
+  else
+    return p * a.decay - m / (__builtin_sqrtf(v * a.r2) + a.eps) * a.rate;
+}
+
+// OV elements of one tensor per lane
+template <typename P, typename G, bool EIGHT, bool FULL>
+__device__ __forceinline__ void adamw_unit(const AdamwArgs& a, const ListEntry& t, float c, uint64_t i, int64_t left) {
+  float g[OV], p[OV], m[OV], v[OV];
+  const uint64_t pos = t.pos + i, blk = pos >> 8;
+  load_up<G, FULL>(t.g, i, left, g);
+  if (t.w32) load_up<float, FULL>(t.w32, i, left, p);
+  else load_up<P, FULL>(t.p, i, left, p);
+  if constexpr (EIGHT) {
+    // the codes of a tensor's last block exist in full
+    uint8_t cm[OV] = {}, cv[OV] = {};
+    int em = 0, ev = 0;
+    if (FULL || left > 0) {
+      __builtin_memcpy(cm, static_cast<const uint8_t*>(a.m) + pos, OV);
+      __builtin_memcpy(cv, static_cast<const uint8_t*>(a.v) + pos, OV);
+      em = 112 + a.em[blk];
+      ev = 96 + a.ev[blk];
+    }
+#pragma unroll
+    for (int k = 0; k < OV; ++k) {
+      const float x = code_up(cm[k] & 127u, em);
+      m[k] = __uint_as_float(__float_as_uint(x) | ((uint32_t)(cm[k] & 128u) << 24));
+      v[k] = code_up(cv[k], ev);
+    }
+  } else {
+    load_up<float, FULL>(a.m, pos, left, m);
+    load_up<float, FULL>(a.v, pos, left, v);
+  }
+  uint32_t tm = 0, tv = 0;
+#pragma unroll
+  for (int k = 0; k < OV; ++k) {
+    const float gc = g[k] * c;
+    m[k] = m[k] * a.b1 + gc * a.a1;
+    v[k] = v[k] * a.b2 + gc * gc * a.a2;
+    p[k] = adamw_p<EIGHT>(a, p[k], m[k], v[k]);
+    if (EIGHT) {
+      // (positions past the tensor's end hold zeros)
+      if (!FULL && k >= left) m[k] = v[k] = 0.0f;
+      const uint32_t bm = __float_as_uint(m[k]) & 0x7FFFFFFFu, bv = __float_as_uint(v[k]);
+      tm = tm > bm ? tm : bm;
+      tv = tv > bv ? tv : bv;
+    }
+  }
+  if (t.w32) store_down<float, FULL>(t.w32, i, left, p);
+  store_down<P, FULL>(t.p, i, left, p);
+  if constexpr (EIGHT) {
+    const int em = block_exponent(half_wave_max(tm)), ev = block_exponent(half_wave_max(tv));
+    uint8_t cm[OV], cv[OV];
+#pragma unroll
+    for (int k = 0; k < OV; k += 2) {
+      // 16 bits of the pair's hash for v, the others for m
+      const uint32_t h = pair_hash((uint32_t)(pos >> 1) + k / 2, a.seed);
+      const uint32_t low = ((h & 0xFFFFu) << 4) | 8u, high = ((h >> 12) & 0xFFFF0u) | 8u;
+      cm[k] = (uint8_t)encode_m(m[k], em, high);
+      cv[k] = (uint8_t)encode_v(v[k], ev, low);
+      cm[k + 1] = (uint8_t)encode_m(m[k + 1], em, low);
+      cv[k + 1] = (uint8_t)encode_v(v[k + 1], ev, high);
+    }
+    if (FULL || left > 0) {
+      __builtin_memcpy(static_cast<uint8_t*>(a.m) + pos, cm, OV);
+      __builtin_memcpy(static_cast<uint8_t*>(a.v) + pos, cv, OV);
+      if ((threadIdx.x & 31u) == 0) {
+        a.em[blk] = (int8_t)em;
+        a.ev[blk] = (int8_t)ev;
+      }
+    }
+  } else {
+    store_down<float, FULL>(a.m, pos, left, m);
+    store_down<float, FULL>(a.v, pos, left, v);
+  }
+}
+
 template <typename P, typename G, bool EIGHT>
 __global__ __launch_bounds__(ONT) void k_adamw(const AdamwArgs a) {
   float c = 1.0f;
@@ -149,82 +234,16 @@ __global__ __launch_bounds__(ONT) void k_adamw(const AdamwArgs a) {
     if (!(__builtin_fabsf(a.clip[0]) < __builtin_inff())) return;
     c = a.clip[1];
   }
-  const uint32_t t = find_tensor(a, blockIdx.x);
-  const uint64_t n = a.t[t].n, pos0 = a.t[t].pos;
-  void* const pp = a.t[t].p;
-  const void* const gp = a.t[t].g;
-  float* const wp = a.t[t].w32;
-  uint64_t i = (uint64_t)(blockIdx.x - a.first[t]) * a.chunk + threadIdx.x * OV;
-  for (uint32_t done = 0; done < a.chunk; done += UNIT, i += UNIT) {
-    const int64_t left = (int64_t)(n - i);
-    // whole wavefronts leave together only where no lane has work
-    if (__ballot(left > 0) == 0) break;
-    float g[OV], p[OV], m[OV], v[OV];
-    const uint64_t pos = pos0 + i;
-    load_up<G>(gp, i, left, g);
-    if (wp) load_up<float>(wp, i, left, p);
-    else load_up<P>(pp, i, left, p);
-    const uint64_t blk = pos >> 8;
-    if constexpr (EIGHT) {
-      // the codes of a tensor's last block exist in full
-      uint8_t cm[OV] = {}, cv[OV] = {};
-      int em = 0, ev = 0;
-      if (left > 0) {
-        __builtin_memcpy(cm, static_cast<const uint8_t*>(a.m) + pos, OV);
-        __builtin_memcpy(cv, static_cast<const uint8_t*>(a.v) + pos, OV);
-        em = 112 + a.em[blk];
-        ev = 96 + a.ev[blk];
-      }
-#pragma unroll
-      for (int k = 0; k < OV; ++k) {
-        const float x = code_up(cm[k] & 127u, em);
-        m[k] = __uint_as_float(__float_as_uint(x) | ((uint32_t)(cm[k] & 128u) << 24));
-        v[k] = code_up(cv[k], ev);
-      }
-    } else {
-      load_up<float>(a.m, pos, left, m);
-      load_up<float>(a.v, pos, left, v);
-    }
-    uint32_t tm = 0, tv = 0;
-#pragma unroll
-    for (int k = 0; k < OV; ++k) {
-      const float gc = g[k] * c;
-      m[k] = m[k] * a.b1 + gc * a.a1;
-      v[k] = v[k] * a.b2 + gc * gc * a.a2;
-      p[k] = p[k] * a.decay - m[k] / (__builtin_sqrtf(v[k] * a.r2) + a.eps) * a.rate;
-      if (EIGHT) {
-        // (positions past the tensor's end hold zeros)
-        if (k >= left) m[k] = v[k] = 0.0f;
-        const uint32_t bm = __float_as_uint(m[k]) & 0x7FFFFFFFu, bv = __float_as_uint(v[k]);
-        tm = tm > bm ? tm : bm;
-        tv = tv > bv ? tv : bv;
-      }
-    }
-    if (wp) store_down<float>(wp, i, left, p);
-    store_down<P>(pp, i, left, p);
-    if constexpr (EIGHT) {
-      const int em = block_exponent(half_wave_max(tm)), ev = block_exponent(half_wave_max(tv));
-      uint8_t cm[OV], cv[OV];
-#pragma unroll
-      for (int k = 0; k < OV; ++k) {
-        const uint32_t h = pair_hash((uint32_t)((pos + k) >> 1), a.seed);
-        // 16 bits of the pair's hash for v, the others for m
-        const uint32_t low = ((h & 0xFFFFu) << 4) | 8u, high = ((h >> 16) << 4) | 8u;
-        cm[k] = (uint8_t)encode_m(m[k], em, (k & 1) ? low : high);
-        cv[k] = (uint8_t)encode_v(v[k], ev, (k & 1) ? high : low);
-      }
-      if (left > 0) {
-        __builtin_memcpy(static_cast<uint8_t*>(a.m) + pos, cm, OV);
-        __builtin_memcpy(static_cast<uint8_t*>(a.v) + pos, cv, OV);
-        if ((threadIdx.x & 31u) == 0) {
-          a.em[blk] = (int8_t)em;
-          a.ev[blk] = (int8_t)ev;
-        }
-      }
-    } else {
-      store_down<float>(a.m, pos, left, m);
-      store_down<float>(a.v, pos, left, v);
-    }
+  const uint32_t k = find_tensor(a, blockIdx.x);
+  const ListEntry t = a.t[k];
+  const uint64_t first = (uint64_t)(blockIdx.x - a.first[k]) * a.chunk;
+  uint64_t i = first + threadIdx.x * OV;
+  if (first + a.chunk <= t.n) {
+    for (uint32_t done = 0; done < a.chunk; done += UNIT, i += UNIT) adamw_unit<P, G, EIGHT, true>(a, t, c, i, OV);
+  } else {
+    // (wavefronts leave whole: the block exponents need all lanes)
+    for (uint32_t done = 0; done < a.chunk && __ballot(i < t.n) != 0; done += UNIT, i += UNIT)
+      adamw_unit<P, G, EIGHT, false>(a, t, c, i, (int64_t)(t.n - i));
   }
 }
 
@@ -265,28 +284,51 @@ hipError_t launch_adamw(int p_dt, int g_dt, int bits, AdamwArgs& a, const ListEn
 }
 
 // ------------------------------------------- 8-bit moments as their values
+// a wavefront takes a block at a time: 4 codes a lane, so that its stores of
+// 16 bytes a lane are 1 KB in a row
+constexpr uint32_t MB = 4;     // blocks of a wavefront
+
 __global__ __launch_bounds__(ONT) void k_moments(const MomentsArgs a) {
-  for (uint64_t i = ((uint64_t)blockIdx.x * ONT + threadIdx.x) * OV; i < a.n; i += (uint64_t)gridDim.x * UNIT) {
-    const uint64_t blk = i >> 8;
-    const int em = 112 + a.em[blk], ev = 96 + a.ev[blk];
-    uint8_t cm[OV], cv[OV];
-    __builtin_memcpy(cm, a.m + i, OV);
-    __builtin_memcpy(cv, a.v + i, OV);
-    float m[OV], v[OV];
+  const uint64_t first = ((uint64_t)blockIdx.x * (ONT / WAVE) + (threadIdx.x >> 6)) * MB;
+  const uint32_t at = (threadIdx.x & 63u) * 4u;
+  uint32_t cm[MB], cv[MB];
+  int em[MB], ev[MB];
 #pragma unroll
-    for (int k = 0; k < OV; ++k) {
-      m[k] = __uint_as_float(__float_as_uint(code_up(cm[k] & 127u, em)) | ((uint32_t)(cm[k] & 128u) << 24));
-      v[k] = code_up(cv[k], ev);
+  for (uint32_t b = 0; b < MB; ++b) {
+    const uint64_t blk = first + b;
+    if (blk >= a.n >> 8) break;
+    __builtin_memcpy(&cm[b], a.m + (blk << 8) + at, 4);
+    __builtin_memcpy(&cv[b], a.v + (blk << 8) + at, 4);
+    em[b] = 112 + a.em[blk];
+    ev[b] = 96 + a.ev[blk];
+  }
+#pragma unroll
+  for (uint32_t b = 0; b < MB; ++b) {
+    const uint64_t blk = first + b;
+    if (blk >= a.n >> 8) break;
+    float m[4], v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t x = cm[b] >> (8 * k);
+      m[k] = __uint_as_float(__float_as_uint(code_up(x & 127u, em[b])) | (x & 128u) << 24);
+      v[k] = code_up((cv[b] >> (8 * k)) & 255u, ev[b]);
     }
-    store_down<float>(a.m_out, i, OV, m);
-    store_down<float>(a.v_out, i, OV, v);
+    put<float, 4>(a.m_out, (blk << 8) + at, m);
+    put<float, 4>(a.v_out, (blk << 8) + at, v);
   }
 }
 
 hipError_t launch_moments(const MomentsArgs& a, hipStream_t st) {
-  const uint64_t units = (a.n + UNIT - 1) / UNIT, most = (uint64_t)device_cus() * 32u;
-  hipLaunchKernelGGL(k_moments, dim3((uint32_t)(units < most ? units : most)), dim3(ONT), 0, st, a);
-  return hipGetLastError();
+  const uint64_t per = (uint64_t)(ONT / WAVE) * MB * 256u;
+  for (uint64_t at = 0; at < a.n;) {
+    const uint64_t n = a.n - at < per << 30 ? a.n - at : per << 30;
+    const MomentsArgs part = {a.m + at, a.v + at, a.em + (at >> 8), a.ev + (at >> 8), a.m_out + at, a.v_out + at, n};
+    hipLaunchKernelGGL(k_moments, dim3((uint32_t)((n + per - 1) / per)), dim3(ONT), 0, st, part);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    at += n;
+  }
+  return hipSuccess;
 }
 
 // -------------------------------------------------------------------- norm
@@ -313,13 +355,23 @@ __global__ __launch_bounds__(ONT) void k_grad_norm(const NormArgs a) {
   for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
     const uint32_t t = find_tensor(a, c);
     const uint64_t n = a.t[t].n, i0 = (uint64_t)(c - a.first[t]) * a.chunk;
+    const uint64_t i = i0 + threadIdx.x * OV;
+    if (i0 + a.chunk <= n) {
+      // (whole units: the loads of four go out together)
 #pragma unroll 4
-    for (uint32_t done = 0; done < a.chunk; done += UNIT) {
-      const uint64_t i = i0 + done + threadIdx.x * OV;
-      float g[OV];
-      load_up<G>(a.t[t].g, i, (int64_t)(n - i), g);
+      for (uint32_t done = 0; done < a.chunk; done += UNIT) {
+        float g[OV];
+        load_up<G, true>(a.t[t].g, i + done, OV, g);
 #pragma unroll
-      for (int k = 0; k < OV; ++k) s += (double)g[k] * (double)g[k];
+        for (int k = 0; k < OV; ++k) s += (double)g[k] * (double)g[k];
+      }
+    } else {
+      for (uint32_t done = 0; done < a.chunk; done += UNIT) {
+        float g[OV];
+        load_up<G, false>(a.t[t].g, i + done, (int64_t)(n - i - done), g);
+#pragma unroll
+        for (int k = 0; k < OV; ++k) s += (double)g[k] * (double)g[k];
+      }
     }
   }
   s = block_sum(s);

@@ -859,6 +859,7 @@ TC_API tc_status tc_adamw_step(const tc_adamw* a, const tc_tensor* list, uint64_
     return fail(TC_ERR_ARG, "beta1 %g, beta2 %g not in [0, 1)", a->beta1, a->beta2);
   if (!(a->eps >= 0.0) || !std::isfinite(a->eps) || !std::isfinite(a->lr) || !std::isfinite(a->weight_decay))
     return fail(TC_ERR_ARG, "lr %g, eps %g, weight_decay %g", a->lr, a->eps, a->weight_decay);
+  if (a->bits == 8 && a->eps < 1e-15) return fail(TC_ERR_ARG, "eps %g is below 1e-15 with 8-bit moments", a->eps);
   if (a->t == 0) return fail(TC_ERR_ARG, "steps are counted from 1");
   const tc_status s = check_list(list, n_list, g_dt, p_dt, true);
   if (s != TC_OK) return s;

@@ -6,8 +6,8 @@ libtc.so (include/tc.h), and there is no fallback."""
 from __future__ import annotations
 
 import ctypes as C
-import math
 
+import numpy as np
 import torch
 
 from . import tc
@@ -94,7 +94,10 @@ class AdamW:
         self.state = state if state is not None else self._zeros()
         self._check_state()
         self.w32 = [p.detach().float() for p in self.params] if master and self.dtype != torch.float32 else None
+        self.sizes = [p.numel() for p in self.params]
         self.table = (tc.Tensor * len(self.params))()
+        # the table's column of gradient addresses, which every step fills in
+        self.g_column = np.frombuffer(self.table, dtype=np.uint64).reshape(len(self.params), -1)[:, 1]
         for k, (row, p) in enumerate(zip(self.table, self.params)):
             row.p, row.n, row.pos = p.data_ptr(), p.numel(), self.places[k]
             row.w32 = self.w32[k].data_ptr() if self.w32 else None
@@ -124,15 +127,16 @@ class AdamW:
             grads = [p.grad for p in self.params]
         if len(grads) != len(self.params):
             raise ValueError(f"{len(grads)} gradients for {len(self.params)} parameters")
+        # (every call's tensors are looked at; one pass per property is the cheapest way)
         gdt, dev = grads[0].dtype, self.device
-        for row, g in zip(self.table, grads):
-            if g.dtype != gdt or g.device != dev:
-                raise TypeError(f"gradients must be of one dtype on {dev}")
-            if g.numel() != row.n or not g.is_contiguous():
-                raise ValueError("a gradient does not fit its parameter, or is not contiguous")
-            row.g = g.data_ptr()
+        at = -1 if dev.index is None else dev.index
+        if [g.get_device() for g in grads] != [at] * len(grads) or {g.dtype for g in grads} != {gdt}:
+            raise TypeError(f"gradients must be of one dtype on {dev}")
+        if [g.numel() for g in grads] != self.sizes or not all([g.is_contiguous() for g in grads]):
+            raise ValueError("a gradient does not fit its parameter, or is not contiguous")
         if gdt not in tc._DT:
             raise TypeError(f"unsupported dtype {gdt}")
+        self.g_column[:] = [g.data_ptr() for g in grads]
         if clip is not None and (clip.dtype != torch.float32 or clip.numel() != 2 or clip.device != dev or
                                  not clip.is_contiguous()):
             raise ValueError(f"clip must be float32 [2] on {dev}")
@@ -152,8 +156,7 @@ class AdamW:
         st = self.state
         if self.bits == 32:
             return st["m"], st["v"]
-        m = torch.empty(self.size, dtype=torch.float32, device=self.device)
-        v = torch.empty_like(m)
+        m, v = torch.empty((2, self.size), dtype=torch.float32, device=self.device)
         tc._need_gpu(m)
         tc._check(tc.lib().tc_adamw_moments(st["m"].data_ptr(), st["em"].data_ptr(), st["v"].data_ptr(),
                                             st["ev"].data_ptr(), self.size, m.data_ptr(), v.data_ptr(),

@@ -93,6 +93,7 @@ def settings(**kw):
     (dict(beta1=1.0), {}, 0, 0, tc.TC_ERR_ARG),
     (dict(beta2=float("nan")), {}, 0, 0, tc.TC_ERR_ARG),
     (dict(eps=-1.0), {}, 0, 0, tc.TC_ERR_ARG),
+    (dict(eps=0.0, bits=8), {}, 0, 0, tc.TC_ERR_ARG),
     (dict(lr=float("inf")), {}, 0, 0, tc.TC_ERR_ARG),
     (dict(m=None), {}, 0, 0, tc.TC_ERR_NULL),
     (dict(bits=8), {}, 0, 0, tc.TC_ERR_NULL),
