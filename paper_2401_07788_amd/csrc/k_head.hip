@@ -77,7 +77,9 @@ template <typename V8, int J> struct Cfg;
 template <typename V8> struct Cfg<V8, 256> : Gemm<V8, 4, 2, 2, 4, 4> { static constexpr uint32_t PER_CU = 1; };
 template <typename V8> struct Cfg<V8, 128> : Gemm<V8, 4, 2, 2, 2, 3> { static constexpr uint32_t PER_CU = 2; };
 template <typename V8> struct Cfg<V8, 64> : Gemm<V8, 2, 2, 4, 1, 4> { static constexpr uint32_t PER_CU = 2; };
-uint32_t tile_tokens(uint64_t rows) { return rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
+// (the loss alone reads w as it is, in the smallest tiles up to 128 tokens:
+// the second one finds w's rows in the cache)
+uint32_t tile_tokens(uint64_t rows, bool direct) { return rows <= (direct ? 128 : 64) ? 64 : rows <= 128 ? 128 : 256; }
 
 // what the first kernels find out about the inputs, on the device
 struct Info {
@@ -104,98 +106,123 @@ __device__ __forceinline__ uint16_t narrow(float v) {
 
 // ------------------------------------------------- tokens that have a target
 // rows: those that have one from the front, in order, the others after them.
-constexpr int RNT = 1024, RE = 8;      // threads; tokens of a thread at once
+// NT threads take NT * RE tokens at a time; place(i, kept, at) is called for
+// each with its place in the list.  Returns how many have a target.
+constexpr int RE = 8;
 
-__global__ __launch_bounds__(RNT) void k_head_rows(const HeadArgs a) {
-  __shared__ uint32_t part[RE][RNT / WAVE], tops[RNT / WAVE], all;
-  static_assert(RE * RNT / WAVE == 128, "two a lane");
+__device__ __forceinline__ bool has_target(const HeadArgs& a, int64_t t) { return t != a.ignore && t >= 0 && (uint64_t)t < a.v; }
+
+template <int NT, typename Place>
+__device__ __forceinline__ uint32_t list_rows(const HeadArgs& a, Place place) {
+  constexpr int COUNTS = RE * NT / WAVE, PER = (COUNTS + 63) / 64;
+  __shared__ uint32_t part[COUNTS], all;
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-  Info* const info = (Info*)a.info;
-  uint32_t top = 0, kept = 0;
-  for (uint64_t i0 = 0; i0 < a.n; i0 += RNT * RE) {
+  uint32_t kept = 0;
+  for (uint64_t i0 = 0; i0 < a.n; i0 += NT * RE) {
     int64_t t[RE];
-    float g[RE];
 #pragma unroll
     for (int e = 0; e < RE; ++e) {
-      const uint64_t i = i0 + e * RNT + threadIdx.x;
+      const uint64_t i = i0 + e * NT + threadIdx.x;
       t[e] = i < a.n ? a.target[i] : a.ignore;
-      g[e] = a.weight && i < a.n ? a.weight[i] : 1.0f;
     }
     uint64_t ones[RE];
-    bool keep[RE];
 #pragma unroll
-    for (int e = 0; e < RE; ++e) {
-      const uint64_t i = i0 + e * RNT + threadIdx.x;
-      keep[e] = i < a.n && t[e] != a.ignore;
-      if (keep[e] && (t[e] < 0 || (uint64_t)t[e] >= a.v)) {
-        raise_error(KERR_BAD_INDEX);
-        keep[e] = false;
-      }
-      if (keep[e]) top = max(top, __float_as_uint(g[e]) & 0x7FFFFFFFu);
-      ones[e] = __ballot(keep[e]);
-    }
+    for (int e = 0; e < RE; ++e) ones[e] = __ballot(has_target(a, t[e]));
     __syncthreads();
     if (lane == 0)
 #pragma unroll
-      for (int e = 0; e < RE; ++e) part[e][wave] = (uint32_t)__popcll(ones[e]);
+      for (int e = 0; e < RE; ++e) part[e * (NT / WAVE) + wave] = (uint32_t)__popcll(ones[e]);
     __syncthreads();
     if (wave == 0) {
-      // exclusive sums over the 128 counts, two a lane
-      uint32_t* const p = &part[0][0] + 2 * lane;
-      const uint32_t x = p[0], y = p[1];
-      uint32_t sum = x + y;
+      // exclusive sums over the counts, PER of them a lane
+      uint32_t c[PER], sum = 0;
+#pragma unroll
+      for (int k = 0; k < PER; ++k) sum += c[k] = lane * PER + k < COUNTS ? part[lane * PER + k] : 0u;
+      const uint32_t own = sum;
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) {
         const uint32_t v = (uint32_t)__shfl_up((int)sum, d);
         if (lane >= (uint32_t)d) sum += v;
       }
-      p[0] = sum - x - y;
-      p[1] = sum - y;
+      uint32_t before = sum - own;
+#pragma unroll
+      for (int k = 0; k < PER; ++k) {
+        if (lane * PER + k < COUNTS) part[lane * PER + k] = before;
+        before += c[k];
+      }
       if (lane == 63) all = sum;
     }
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < RE; ++e) {
-      const uint64_t i = i0 + e * RNT + threadIdx.x;
-      const uint32_t mine = kept + part[e][wave] + (uint32_t)__popcll(ones[e] & ((1ull << lane) - 1));   // kept tokens before token i
-      if (keep[e]) a.rows[mine] = (uint32_t)i;
-      else if (i < a.n) {
-        a.rows[(uint32_t)a.n - 1u - ((uint32_t)i - mine)] = (uint32_t)i;
-        a.loss[i] = a.lse[i] = 0.0f;
-      }
+      const uint64_t i = i0 + e * NT + threadIdx.x;
+      // kept tokens before token i
+      const uint32_t mine = kept + part[e * (NT / WAVE) + wave] + (uint32_t)__popcll(ones[e] & ((1ull << lane) - 1));
+      const bool keep = ones[e] >> lane & 1u;
+      if (i < a.n) place((uint32_t)i, keep, keep ? mine : (uint32_t)a.n - 1u - ((uint32_t)i - mine));
     }
     kept += all;
   }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-  if (lane == 0) tops[wave] = top;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (uint32_t k = 0; k < RNT / WAVE; ++k) top = max(top, tops[k]);
-    info->count = kept;
-    info->top_g = top;
-    info->top_x = info->top_w = 0;
-  }
+  return kept;
 }
 
-// largest magnitude of x's listed rows (blockIdx.y 0) and of w (a maximum: any
-// order gives it)
-__global__ __launch_bounds__(256) void k_head_top(const HeadArgs a) {
-  __shared__ uint32_t part[4];
-  Info* const info = (Info*)a.info;
-  const bool of_w = blockIdx.y != 0;
-  const uint64_t rows = of_w ? a.v : info->count;
-  uint32_t top = 0;
-  for (uint64_t r = blockIdx.x * 4u + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4u) {
-    const float* p = of_w ? (const float*)a.w + r * a.ldw : (const float*)a.x + a.rows[r] * a.ldx;
-#pragma unroll 8
-    for (uint32_t k = threadIdx.x & 63u; k < a.h; k += 64) top = max(top, __float_as_uint(p[k]) & 0x7FFFFFFFu);
-  }
+// largest of a workgroup's values, in every thread
+template <int NT>
+__device__ __forceinline__ uint32_t block_max(uint32_t v) {
+  __shared__ uint32_t part[NT / WAVE];
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-  if ((threadIdx.x & 63u) == 0) part[threadIdx.x >> 6] = top;
+  for (int d = 32; d > 0; d >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
   __syncthreads();
-  if (threadIdx.x == 0) atomicMax(of_w ? &info->top_w : &info->top_x, max(max(part[0], part[1]), max(part[2], part[3])));
+  if ((threadIdx.x & 63u) == 0) part[threadIdx.x >> 6] = v;
+  __syncthreads();
+  for (int k = 0; k < NT / WAVE; ++k) v = max(v, part[k]);
+  return v;
+}
+
+// The list as the other kernels read it, zero losses for the others, and the
+// largest weight.
+template <int NT>
+__device__ __forceinline__ uint32_t write_rows(const HeadArgs& a) {
+  uint32_t top = 0;
+  const uint32_t kept = list_rows<NT>(a, [&](uint32_t i, bool keep, uint32_t at) {
+    a.rows[at] = i;
+    if (keep) {
+      top = max(top, a.weight ? __float_as_uint(a.weight[i]) & 0x7FFFFFFFu : 0x3F800000u);
+    } else {
+      a.loss[i] = a.lse[i] = 0.0f;
+      if (a.target[i] != a.ignore) raise_error(KERR_BAD_INDEX);
+    }
+  });
+  top = block_max<NT>(top);
+  if (threadIdx.x == 0) {
+    ((Info*)a.info)->count = kept;
+    ((Info*)a.info)->top_g = top;
+  }
+  return kept;
+}
+
+// The first workgroup lists the tokens; for binary32 the others find the
+// largest magnitudes of x's rows that have a target and of w, one for each of
+// top_x and top_w workgroups (k_head_pack joins them).
+constexpr int BNT = 1024;
+
+__global__ __launch_bounds__(BNT) void k_head_begin(const HeadArgs a) {
+  if (blockIdx.x == 0) {
+    write_rows<BNT>(a);
+    return;
+  }
+  const uint32_t b = blockIdx.x - 1u, lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+  const bool of_w = b >= a.top_x;
+  const uint64_t rows = of_w ? a.v : a.n, first = of_w ? b - a.top_x : b, step = (of_w ? a.top_w : a.top_x) * (uint64_t)(BNT / WAVE);
+  uint32_t top = 0;
+  for (uint64_t r = first * (BNT / WAVE) + wave; r < rows; r += step) {
+    if (!of_w && !has_target(a, a.target[r])) continue;
+    const float* p = of_w ? (const float*)a.w + r * a.ldw : (const float*)a.x + r * a.ldx;
+#pragma unroll 8
+    for (uint32_t k = lane; k < a.h; k += 64) top = max(top, __float_as_uint(p[k]) & 0x7FFFFFFFu);
+  }
+  top = block_max<BNT>(top);
+  if (threadIdx.x == 0) a.tops[b] = top;
 }
 
 // ------------------------------------------------------ operands laid out
@@ -205,17 +232,14 @@ __global__ __launch_bounds__(256) void k_head_top(const HeadArgs a) {
 constexpr uint32_t PACK_KB = 16;
 
 template <typename T, bool OF_W>
-__device__ __forceinline__ void pack_rows(const HeadArgs& a, uint32_t c0, uint32_t block) {
+__device__ __forceinline__ void pack_rows(const HeadArgs& a, uint32_t rows, const uint32_t* list, uint32_t top, uint32_t rb, uint32_t kb0) {
   using R = typename Elem<T>::raw;
   constexpr int PL = Type<T>::PLANES;
-  const Info info = *(const Info*)a.info;
-  const uint32_t wide = (a.k_logits + PACK_KB - 1) / PACK_KB, rb = block / wide, kb0 = block % wide * PACK_KB;
-  const uint32_t rows = OF_W ? (uint32_t)a.v : chunk_tokens(a, c0);
   if (rb * 16u >= (rows + KSTAGE - 1) / KSTAGE * KSTAGE) return;
-  const int e = PL == 2 ? plane_exp(OF_W ? info.top_w : info.top_x) : 0;
+  const int e = PL == 2 ? plane_exp(top) : 0;
   const uint32_t lane = threadIdx.x & 63u, row = lane >> 2, piece = (lane & 3u) ^ turn(row), r = rb * 16u + row;
   const R* src = nullptr;
-  if (r < rows) src = (const R*)(OF_W ? a.w : a.x) + (uint64_t)(OF_W ? r : a.rows[c0 + r]) * (OF_W ? a.ldw : a.ldx);
+  if (r < rows) src = (const R*)(OF_W ? a.w : a.x) + (uint64_t)(OF_W ? r : list[row]) * (OF_W ? a.ldw : a.ldx);
   struct __attribute__((packed, aligned(sizeof(R)))) Run { R v[8]; };
 #pragma unroll
   for (uint32_t q = 0; q < PACK_KB / 4; ++q) {
@@ -246,11 +270,44 @@ __device__ __forceinline__ void pack_rows(const HeadArgs& a, uint32_t c0, uint32
   }
 }
 
-// the first `of_w` workgroups lay out w, the others the chunk's tokens
-template <typename T>
+// The first `of_w` workgroups lay out w, the others the chunk's tokens.
+// ALONE: there is no k_head_begin before it; with few tokens each workgroup
+// lists them for itself, which takes less time than a launch.
+constexpr uint32_t ALONE_TOKENS = 256 * RE;
+
+template <typename T, bool ALONE>
 __global__ __launch_bounds__(256) void k_head_pack(const HeadArgs a, uint32_t c0, uint32_t of_w) {
-  if (blockIdx.x < of_w) pack_rows<T, true>(a, c0, blockIdx.x);
-  else pack_rows<T, false>(a, c0, blockIdx.x - of_w);
+  __shared__ uint32_t list[16];
+  const uint32_t wide = (a.k_logits + PACK_KB - 1) / PACK_KB;
+  const bool is_w = blockIdx.x < of_w;
+  const uint32_t b = is_w ? blockIdx.x : blockIdx.x - of_w, rb = b / wide, kb0 = b % wide * PACK_KB;
+  uint32_t top = 0;
+  if constexpr (Type<T>::PLANES == 2) {
+    // (the last workgroup leaves both for the kernels after this one)
+    const uint32_t x = block_max<256>(threadIdx.x < a.top_x ? a.tops[threadIdx.x] : 0u);
+    const uint32_t w = block_max<256>(threadIdx.x < a.top_w ? a.tops[a.top_x + threadIdx.x] : 0u);
+    top = is_w ? w : x;
+    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) {
+      ((Info*)a.info)->top_x = x;
+      ((Info*)a.info)->top_w = w;
+    }
+  }
+  if (is_w) {
+    pack_rows<T, true>(a, (uint32_t)a.v, nullptr, top, rb, kb0);
+    return;
+  }
+  uint32_t rows;
+  if constexpr (ALONE) {
+    if (b == 0) write_rows<256>(a);
+    rows = list_rows<256>(a, [&](uint32_t i, bool keep, uint32_t at) {
+      if (keep && at >> 4 == rb) list[at & 15u] = i;
+    });
+  } else {
+    rows = chunk_tokens(a, c0);
+    if (threadIdx.x < 16 && rb * 16u + threadIdx.x < rows) list[threadIdx.x] = a.rows[c0 + rb * 16u + threadIdx.x];
+  }
+  __syncthreads();
+  pack_rows<T, false>(a, rows, list, top, rb, kb0);
 }
 
 // ---------------------------------------------------------------- the logits
@@ -387,12 +444,23 @@ __global__ __launch_bounds__(SNT) void k_head_loss(const HeadArgs a, uint32_t c0
   if (blockIdx.x * SR >= left) return;
   float m = -__builtin_inff(), s = 0.0f;
   if (j < left) {
-#pragma unroll 4
-    for (uint32_t p = q; p < pieces; p += SNT / SR) {
-      const float2 v = a.stats[(uint64_t)p * a.chunk + j];
-      const float top = fmaxf(m, v.x);
-      // (a piece whose logits are all -inf adds nothing)
-      if (top > -__builtin_inff()) s = s * __expf(m - top) + v.y * __expf(v.x - top);
+    constexpr uint32_t B = 8;         // pieces at a time: their loads go out together
+    for (uint32_t p = q; p < pieces; p += B * (SNT / SR)) {
+      float2 v[B];
+      float top = m;
+#pragma unroll
+      for (uint32_t k = 0; k < B; ++k) {
+        const uint32_t at = p + k * (SNT / SR);
+        v[k] = at < pieces ? a.stats[(uint64_t)at * a.chunk + j] : make_float2(-__builtin_inff(), 0.0f);
+      }
+#pragma unroll
+      for (uint32_t k = 0; k < B; ++k) top = fmaxf(top, v[k].x);
+      // (pieces whose logits are all -inf add nothing)
+      if (top > -__builtin_inff()) {
+        s *= __expf(m - top);
+#pragma unroll
+        for (uint32_t k = 0; k < B; ++k) s += v[k].y * __expf(v[k].x - top);
+      }
       m = top;
     }
   }
@@ -423,12 +491,11 @@ __global__ __launch_bounds__(SNT) void k_head_loss(const HeadArgs a, uint32_t c0
 }
 
 // --------------------------------- d: softmax minus target, times the weight
-// A workgroup takes 128 tokens by 256 vocabulary entries, a lane half a row of
-// a block (32 bytes) at a time: one pass over the memory, bound by it.
-constexpr uint32_t SOFT_KB = 8;
+// A workgroup takes 128 tokens by up to 256 vocabulary entries, a lane half a
+// row of a block (32 bytes) at a time: one pass over the memory, bound by it.
 
 template <typename T, int J>
-__global__ __launch_bounds__(256) void k_head_softmax(const HeadArgs a, uint32_t c0, uint32_t piece_bits) {
+__global__ __launch_bounds__(256) void k_head_softmax(const HeadArgs a, uint32_t c0, uint32_t piece_bits, uint32_t blocks) {
   constexpr int PL = Type<T>::PLANES;
   using N = Numerator<T, WIDE<T, J>>;
   using R = typename N::R;
@@ -440,7 +507,7 @@ __global__ __launch_bounds__(256) void k_head_softmax(const HeadArgs a, uint32_t
   const uint32_t goal = __float_as_uint(row.z);
   const float w = row.y * P_SCALE<T>;
 #pragma unroll 2
-  for (uint32_t kb = blockIdx.x * SOFT_KB; kb < min(a.k_dx, blockIdx.x * SOFT_KB + SOFT_KB); ++kb) {
+  for (uint32_t kb = blockIdx.x * blocks; kb < min(a.k_dx, blockIdx.x * blocks + blocks); ++kb) {
     const uint64_t at = ((uint64_t)kb * a.c_blocks + (j >> 4)) * 64u + (j & 15u) * 4u;    // in pieces
     uint16_t v[PL][16] = {};
     if (in) {
@@ -468,21 +535,38 @@ __global__ __launch_bounds__(256) void k_head_softmax(const HeadArgs a, uint32_t
 }
 
 // ------------------------------------------------------------- the gradients
-// dx of the chunk's tokens: sums over `splits` parts of the vocabulary
+// dx of the chunk's tokens: sums over parts of the vocabulary.  The host
+// chose their number for a full chunk; where tokens without a target left
+// fewer tiles than workgroups, the tokens that are left have room for more.
+struct DxPlan {
+  uint32_t ni, nj, all, splits;
+  __device__ __forceinline__ DxPlan(const HeadArgs& a, uint32_t left, uint32_t ti, uint32_t tj, uint32_t pairs) {
+    ni = (a.h + ti - 1) / ti;
+    nj = (left + tj - 1) / tj;
+    all = pairs * a.k_dx;
+    splits = a.splits;
+    const uint32_t tiles = max(ni * nj, 1u), room = (uint32_t)min((uint64_t)a.splits * a.chunk / max(left, 1u), (uint64_t)max(all / 16u, 1u));
+    const uint32_t more = min(a.dx_grid / tiles, room);
+    // (rounds of tiles, by the length of a part)
+    auto rounds = [&](uint32_t s) { return (tiles * s + a.dx_grid - 1) / a.dx_grid; };
+    if (more > splits && (uint64_t)rounds(more) * splits < (uint64_t)rounds(splits) * more) splits = more;
+  }
+};
+
 template <typename T, int J>
 __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_dx(const HeadArgs a, uint32_t c0) {
   using G = Cfg<typename Type<T>::V8, J>;
   extern __shared__ __attribute__((aligned(128))) char lds[];
   const uint32_t left = chunk_tokens(a, c0);
-  const uint32_t ni = (a.h + G::TI - 1) / G::TI, nj = (left + G::TJ - 1) / G::TJ;
-  const uint32_t all = (Type<T>::PLANES == 2 ? 3 : 1) * a.k_dx;
+  const DxPlan plan(a, left, G::TI, G::TJ, Type<T>::PLANES == 2 ? 3 : 1);
+  const uint32_t tiles = plan.ni * plan.nj, all = plan.all, splits = plan.splits;
   auto work = [&](uint32_t n, typename G::Work& w) {
     uint32_t t;
-    if (!nth_tile(n, ni * nj * a.splits, t)) return false;
+    if (!nth_tile(n, tiles * splits, t)) return false;
     // a part's tiles together: they share its rows of w and of d
-    const uint32_t split = t / (ni * nj);
-    const Tile tile = tile_of(t - split * ni * nj, ni, nj);
-    const uint32_t s0 = (uint32_t)((uint64_t)all * split / a.splits), s1 = (uint32_t)((uint64_t)all * (split + 1) / a.splits);
+    const uint32_t split = t / tiles;
+    const Tile tile = tile_of(t - split * tiles, plan.ni, plan.nj);
+    const uint32_t s0 = (uint32_t)((uint64_t)all * split / splits), s1 = (uint32_t)((uint64_t)all * (split + 1) / splits);
     w = {tile.i * G::TI, tile.j * G::TJ, s0, s1 - s0};
     return true;
   };
@@ -490,15 +574,15 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h = lane >> 5;
     const uint32_t iw = at.i0 + (wave % G::NWI) * (G::WI * 32) + h * 16, jw = at.j0 + (wave / G::NWI) * (G::WJ * 32) + (lane & 31u);
     // (the part that starts at s0: the first that does not end before it)
-    uint32_t split = (uint32_t)((uint64_t)at.s0 * a.splits / all);
-    if ((uint64_t)all * split / a.splits != at.s0) ++split;
+    uint32_t split = (uint32_t)((uint64_t)at.s0 * splits / all);
+    if ((uint64_t)all * split / splits != at.s0) ++split;
 #pragma unroll
     for (int y = 0; y < G::WJ; ++y)
 #pragma unroll
       for (int x = 0; x < G::WI; ++x) {
         const uint32_t i = iw + x * 32, j = jw + y * 32;
         if (i >= a.hq || j >= left) continue;
-        float4* o = reinterpret_cast<float4*>(a.dx_part + ((uint64_t)split * a.chunk + j) * a.hq + i);
+        float4* o = reinterpret_cast<float4*>(a.dx_part + ((uint64_t)split * left + j) * a.hq + i);
 #pragma unroll
         for (int q = 0; q < 4; ++q)
           o[q] = make_float4(acc[x][y][q * 4], acc[x][y][q * 4 + 1], acc[x][y][q * 4 + 2], acc[x][y][q * 4 + 3]);
@@ -513,7 +597,7 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
 // for a token that the model is sure of, dx is a small difference and that
 // entry's rounding would be most of its error.
 template <typename T>
-__global__ __launch_bounds__(256) void k_head_dx_sum(const HeadArgs a, uint32_t c0) {
+__global__ __launch_bounds__(256) void k_head_dx_sum(const HeadArgs a, uint32_t c0, uint32_t tj) {
   using R = typename Elem<T>::raw;
   const Info info = *(const Info*)a.info;
   const uint32_t j = blockIdx.x, i = a.rows[c0 + j];
@@ -526,11 +610,13 @@ __global__ __launch_bounds__(256) void k_head_dx_sum(const HeadArgs a, uint32_t 
   float f = 1.0f / P_SCALE<T>;
   if (!std::is_same_v<T, bf16_t>) f *= __uint_as_float(info.top_g);
   if (Type<T>::PLANES == 2) f = __builtin_ldexpf(f, -plane_exp(info.top_w));
+  const uint32_t left = chunk_tokens(a, c0), splits = DxPlan(a, left, 256, tj, Type<T>::PLANES == 2 ? 3 : 1).splits;
   const float rest = Type<T>::PLANES == 1 ? a.rest[j] : 0.0f;
   const R* w = (const R*)a.w + (uint64_t)a.target[i] * a.ldw;
   for (uint32_t k = threadIdx.x; k < a.h; k += 256) {
     float s = 0.0f;
-    for (uint32_t q = 0; q < a.splits; ++q) s += a.dx_part[((uint64_t)q * a.chunk + j) * a.hq + k];
+#pragma unroll 4
+    for (uint32_t q = 0; q < splits; ++q) s += a.dx_part[((uint64_t)q * left + j) * a.hq + k];
     if (Type<T>::PLANES == 1) s += rest * Elem<T>::up(w[k]);
     o[k] = Elem<T>::down(s * f);
   }
@@ -549,7 +635,7 @@ struct DwPlan {
   __device__ __forceinline__ DwPlan(const HeadArgs& a, uint32_t left) {
     ni = (a.h + G::TI - 1) / G::TI;
     nj = ((uint32_t)a.v + G::TJ - 1) / G::TJ;
-    whole = ni * nj / a.dw_grid * a.dw_grid;
+    whole = a.dw_parts ? ni * nj / a.dw_grid * a.dw_grid : ni * nj;
     rest = ni * nj - whole;
     all = (Type<T>::PLANES == 2 ? 3 : 1) * ((left + KSTAGE - 1) / KSTAGE);
     parts = min(a.dw_parts, all);       // (each has a stage at least)
@@ -581,7 +667,9 @@ __device__ __forceinline__ void dw_store(const HeadArgs& a, uint32_t c0, float f
     for (int r = 0; r < 16; ++r) w[r] = Elem<T>::down(v[r] * f);
     R* o = (R*)a.dw + (uint64_t)j * a.h + i;
     if (i + 16 <= a.h) {
-      store_run<R, 16>(o, w);
+      // (the hardware stores vectors at any element's address)
+      struct __attribute__((packed, aligned(sizeof(R)))) Run { R v[16]; };
+      *reinterpret_cast<Run*>(o) = __builtin_bit_cast(Run, w);
     } else {
 #pragma unroll
       for (int r = 0; r < 16; ++r)
@@ -612,7 +700,7 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, 256>::NT), 2) void k_hea
   auto done = [&](uint32_t n, const typename G::Work& at, f32x16 (&acc)[G::WI][G::WJ]) {
     const uint32_t iw = at.i0 + (wave % G::NWI) * (G::WI * 32) + h * 16, jw = at.j0 + (wave / G::NWI) * (G::WJ * 32) + (lane & 31u);
     // (of no stages: the zeros of a chunk without tokens)
-    const bool part = at.count != 0 && n * gridDim.x >= plan.whole;
+    const bool part = at.count != 0 && a.dw_parts && n * gridDim.x >= plan.whole;
 #pragma unroll
     for (int y = 0; y < G::WJ; ++y)
 #pragma unroll
@@ -641,7 +729,9 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, 256>::NT), 2) void k_hea
   }
   auto work = [&](uint32_t n, typename G::Work& w) {
     uint32_t t = n * gridDim.x + mine, s0 = 0, s1 = plan.all;
-    if (n * gridDim.x >= plan.whole) {
+    if (!a.dw_parts) {
+      if (t >= plan.whole) return false;
+    } else if (n * gridDim.x >= plan.whole) {
       if (n * gridDim.x > plan.whole || mine >= plan.rest * plan.parts) return false;
       const uint32_t split = mine / plan.rest;
       t = plan.whole + mine - split * plan.rest;
@@ -719,6 +809,10 @@ uint32_t grid_of(uint64_t tiles) {
   return (uint32_t)std::min<uint64_t>(room, (tiles + 7) / 8 * 8);
 }
 
+// whether k_head_pack lists the tokens by itself
+template <typename T>
+bool alone(const HeadArgs& a) { return Type<T>::PLANES == 1 && a.n <= ALONE_TOKENS && a.n <= a.chunk; }
+
 template <typename T, int J, bool GRAD>
 hipError_t chunk_of(HeadArgs& a, uint32_t c0, uint32_t rows, hipStream_t st) {
   using G = Cfg<typename Type<T>::V8, J>;
@@ -727,9 +821,14 @@ hipError_t chunk_of(HeadArgs& a, uint32_t c0, uint32_t rows, hipStream_t st) {
   constexpr uint32_t PIECE = G::WI * 32;
   const uint32_t pieces = ((uint32_t)a.v + PIECE - 1) / PIECE;
   const uint32_t wide = (a.k_logits + PACK_KB - 1) / PACK_KB, of_w = a.wr && c0 == 0 ? a.k_dx * 2 * wide : 0;
-  hipLaunchKernelGGL((k_head_pack<T>), dim3(of_w + (rows + 31) / 32 * 2 * wide), dim3(256), 0, st, a, c0, of_w);
+  const dim3 pack(of_w + (rows + 31) / 32 * 2 * wide);
+  if (alone<T>(a)) {
+    if constexpr (Type<T>::PLANES == 1) hipLaunchKernelGGL((k_head_pack<T, true>), pack, dim3(256), 0, st, a, c0, of_w);
+  } else {
+    hipLaunchKernelGGL((k_head_pack<T, false>), pack, dim3(256), 0, st, a, c0, of_w);
+  }
   HEAD_TRY(hipGetLastError());
-  if constexpr (!GRAD && Type<T>::PLANES == 1) {
+  if constexpr (!GRAD && Type<T>::PLANES == 1 && J != 128) {
     if (!a.wr) {
       HEAD_TRY((launch_lds<k_head_logits<T, J, false, true>>(grid_of<G>(ni * nj), G::NT, G::LDS, st, a, c0)));
     } else {
@@ -742,13 +841,13 @@ hipError_t chunk_of(HeadArgs& a, uint32_t c0, uint32_t rows, hipStream_t st) {
                      !std::is_same_v<T, bf16_t>);
   HEAD_TRY(hipGetLastError());
   if constexpr (GRAD) {
-    hipLaunchKernelGGL((k_head_softmax<T, J>), dim3((a.k_dx + SOFT_KB - 1) / SOFT_KB, (rows + 127) / 128), dim3(256), 0, st, a, c0,
-                       PIECE == 128 ? 7u : 6u);
+    const uint32_t high = (rows + 127) / 128, blocks = std::max(1u, std::min(8u, a.k_dx * high / 2048u));
+    hipLaunchKernelGGL((k_head_softmax<T, J>), dim3((a.k_dx + blocks - 1) / blocks, high), dim3(256), 0, st, a, c0,
+                       PIECE == 128 ? 7u : 6u, blocks);
     HEAD_TRY(hipGetLastError());
-    const uint32_t nh = (a.h + G::TI - 1) / G::TI;
-    HEAD_TRY((launch_lds<k_head_dx<T, J>>(grid_of<G>((uint64_t)nh * nj * a.splits), G::NT, G::LDS, st, a, c0)));
+    HEAD_TRY((launch_lds<k_head_dx<T, J>>(a.dx_grid, G::NT, G::LDS, st, a, c0)));
     if (a.n > 0) {
-      hipLaunchKernelGGL((k_head_dx_sum<T>), dim3(rows), dim3(256), 0, st, a, c0);
+      hipLaunchKernelGGL((k_head_dx_sum<T>), dim3(rows), dim3(256), 0, st, a, c0, G::TJ);
       HEAD_TRY(hipGetLastError());
     }
     using W = Cfg<typename Type<T>::V8, 256>;
@@ -764,17 +863,15 @@ hipError_t chunk_of(HeadArgs& a, uint32_t c0, uint32_t rows, hipStream_t st) {
 
 template <typename T>
 hipError_t head_of(HeadArgs& a, bool grad, hipStream_t st) {
-  hipLaunchKernelGGL(k_head_rows, dim3(1), dim3(RNT), 0, st, a);
-  HEAD_TRY(hipGetLastError());
-  if (Type<T>::PLANES == 2) {
-    hipLaunchKernelGGL(k_head_top, dim3(512, 2), dim3(256), 0, st, a);
+  if (!alone<T>(a)) {
+    hipLaunchKernelGGL(k_head_begin, dim3(1 + (Type<T>::PLANES == 2 ? a.top_x + a.top_w : 0)), dim3(BNT), 0, st, a);
     HEAD_TRY(hipGetLastError());
   }
   // (without a token one chunk still writes a dw of zeros)
   for (uint64_t c0 = 0; c0 == 0 || c0 < a.n; c0 += a.chunk) {
     const uint32_t rows = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(a.chunk, a.n - c0));
     // (one choice for every chunk: the buffers go by it)
-    const uint32_t tokens = tile_tokens(a.chunk), c = (uint32_t)c0;
+    const uint32_t tokens = tile_tokens(a.chunk, !a.wr), c = (uint32_t)c0;
     HEAD_TRY(tokens == 64    ? (grad ? chunk_of<T, 64, true>(a, c, rows, st) : chunk_of<T, 64, false>(a, c, rows, st))
              : tokens == 128 ? (grad ? chunk_of<T, 128, true>(a, c, rows, st) : chunk_of<T, 128, false>(a, c, rows, st))
                              : (grad ? chunk_of<T, 256, true>(a, c, rows, st) : chunk_of<T, 256, false>(a, c, rows, st)));
@@ -818,6 +915,10 @@ uint64_t head_plan(HeadArgs& a, int dt, bool grad, char* base) {
   };
   a.info = take(sizeof(Info));
   a.rows = (uint32_t*)take(a.n * 4);
+  // (up to 256 maxima of x and of w: k_head_pack has a thread for each)
+  a.top_x = planes == 2 ? (uint32_t)std::min<uint64_t>(128, (a.n + 63) / 64) : 0;
+  a.top_w = planes == 2 ? (uint32_t)std::min<uint64_t>(256, (a.v + 63) / 64) : 0;
+  a.tops = (uint32_t*)take((a.top_x + a.top_w) * 4);
   a.zt = (float*)take(a.chunk * 4);
   a.stats = (float2*)take((a.v + 63) / 64 * a.chunk * 8);
   // (a tile of 256 rows of the transposed operand: 8 blocks along k)
@@ -834,7 +935,7 @@ uint64_t head_plan(HeadArgs& a, int dt, bool grad, char* base) {
     a.rest = (float*)take(a.chunk * 4);
     // dx: parts of the vocabulary, as many as cost least: rounds of tiles
     // (about half a microsecond a stage) and the parts' sums written and read
-    const uint64_t tj = tile_tokens(a.chunk), tiles = (a.h + 255) / 256 * ((a.chunk + tj - 1) / tj);
+    const uint64_t tj = tile_tokens(a.chunk, false), tiles = (a.h + 255) / 256 * ((a.chunk + tj - 1) / tj);
     const uint64_t stages = (planes == 2 ? 3 : 1) * (uint64_t)a.k_dx, room = (tj == 256 ? 1 : 2) * (uint64_t)device_cus();
     double best = 0.0;
     a.splits = 0;
@@ -847,11 +948,12 @@ uint64_t head_plan(HeadArgs& a, int dt, bool grad, char* base) {
       }
     }
     a.dx_part = (float*)take(a.splits * a.chunk * a.hq * 4);
+    a.dx_grid = (uint32_t)((std::min(room, tiles * std::max<uint64_t>(stages / 16, 1)) + 7) / 8 * 8);
     // dw: the tiles past the last whole round in as many parts as fill one
     const uint64_t wt = (a.h + 255) / 256 * ((a.v + 255) / 256), cus = (uint64_t)(device_cus() + 7) / 8 * 8;
     a.dw_grid = (uint32_t)std::min<uint64_t>(cus, (wt + 7) / 8 * 8);
     const uint64_t rest = wt % a.dw_grid;
-    a.dw_parts = rest ? (uint32_t)std::min<uint64_t>(a.dw_grid / rest, 16) : 0;
+    a.dw_parts = rest && a.dw_grid >= 2 * rest ? (uint32_t)std::min<uint64_t>(a.dw_grid / rest, 16) : 0;
     a.dw_part = (float*)take(rest * a.dw_parts * 256 * 256 * 4);
     a.dw_sum = one ? nullptr : (float*)take(a.v * a.hq * 4);
   }

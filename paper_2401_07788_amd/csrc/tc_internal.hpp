@@ -175,11 +175,14 @@ struct HeadArgs {
   uint64_t chunk;        // tokens whose softmax is held at once (0: head_plan chooses)
   // head_plan
   uint64_t hq;           // h rounded up to 16
-  uint32_t k_logits, k_dx, splits;              // stages of 32 along h and along v; parts of dx's sum
+  uint32_t k_logits, k_dx;                      // stages of 32 along h and along v
+  uint32_t splits, dx_grid;                     // parts of dx's sum; workgroups of its product
+  uint32_t top_x, top_w;                        // maxima of x and of w in `tops` (binary32)
   uint32_t v_blocks, c_blocks;                  // row blocks of 16, up to whole tiles
   uint64_t wr_plane, xr_plane, pr_plane;        // bytes
   char* info;
-  uint32_t* rows;        // [n] tokens that have a target
+  uint32_t* rows;        // [n] tokens that have a target, then the others
+  uint32_t* tops;
   float* zt;             // [chunk] logit of the target
   float4* row_info;      // [chunk] lse, weight, target (gradients only)
   float* rest;           // [chunk] what rounding took from d's entry at the target
