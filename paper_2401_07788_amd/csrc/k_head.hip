@@ -72,14 +72,14 @@ template <typename T> struct Numerator<T, true> {
 template <typename T, int J> constexpr bool WIDE = J == 64 || std::is_same_v<T, float>;
 
 template <typename V8, int J> struct Cfg;
-// 256 x 256, one workgroup of 8 wavefronts per compute unit; for fewer tokens
-// 256 x 128 and 256 x 64, two of 4 wavefronts
+// 256 x 256, one workgroup of 8 wavefronts per compute unit.  For fewer tokens
+// 128 x 128 and 128 x 64, two of 4 and 2 wavefronts: those products are bound
+// by reading w, and with 256-row tiles a vocabulary of 32000 keeps half of the
+// device busy (one token, h 4096: 70 us, with 128 rows 54 us, 4.8 TB/s).
 template <typename V8> struct Cfg<V8, 256> : Gemm<V8, 4, 2, 2, 4, 4> { static constexpr uint32_t PER_CU = 1; };
-template <typename V8> struct Cfg<V8, 128> : Gemm<V8, 4, 2, 2, 2, 3> { static constexpr uint32_t PER_CU = 2; };
-template <typename V8> struct Cfg<V8, 64> : Gemm<V8, 2, 2, 4, 1, 4> { static constexpr uint32_t PER_CU = 2; };
-// (the loss alone reads w as it is, in the smallest tiles up to 128 tokens:
-// the second one finds w's rows in the cache)
-uint32_t tile_tokens(uint64_t rows, bool direct) { return rows <= (direct ? 128 : 64) ? 64 : rows <= 128 ? 128 : 256; }
+template <typename V8> struct Cfg<V8, 128> : Gemm<V8, 2, 2, 2, 2, 4> { static constexpr uint32_t PER_CU = 2; };
+template <typename V8> struct Cfg<V8, 64> : Gemm<V8, 2, 2, 2, 1, 6> { static constexpr uint32_t PER_CU = 2; };
+uint32_t tile_tokens(uint64_t rows) { return rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
 
 // what the first kernels find out about the inputs, on the device
 struct Info {
@@ -506,7 +506,7 @@ __global__ __launch_bounds__(256) void k_head_softmax(const HeadArgs a, uint32_t
   const float4 row = in ? a.row_info[j] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   const uint32_t goal = __float_as_uint(row.z);
   const float w = row.y * P_SCALE<T>;
-#pragma unroll 2
+#pragma unroll 4
   for (uint32_t kb = blockIdx.x * blocks; kb < min(a.k_dx, blockIdx.x * blocks + blocks); ++kb) {
     const uint64_t at = ((uint64_t)kb * a.c_blocks + (j >> 4)) * 64u + (j & 15u) * 4u;    // in pieces
     uint16_t v[PL][16] = {};
@@ -597,7 +597,7 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
 // for a token that the model is sure of, dx is a small difference and that
 // entry's rounding would be most of its error.
 template <typename T>
-__global__ __launch_bounds__(256) void k_head_dx_sum(const HeadArgs a, uint32_t c0, uint32_t tj) {
+__global__ __launch_bounds__(256) void k_head_dx_sum(const HeadArgs a, uint32_t c0, uint32_t ti, uint32_t tj) {
   using R = typename Elem<T>::raw;
   const Info info = *(const Info*)a.info;
   const uint32_t j = blockIdx.x, i = a.rows[c0 + j];
@@ -610,7 +610,7 @@ __global__ __launch_bounds__(256) void k_head_dx_sum(const HeadArgs a, uint32_t 
   float f = 1.0f / P_SCALE<T>;
   if (!std::is_same_v<T, bf16_t>) f *= __uint_as_float(info.top_g);
   if (Type<T>::PLANES == 2) f = __builtin_ldexpf(f, -plane_exp(info.top_w));
-  const uint32_t left = chunk_tokens(a, c0), splits = DxPlan(a, left, 256, tj, Type<T>::PLANES == 2 ? 3 : 1).splits;
+  const uint32_t left = chunk_tokens(a, c0), splits = DxPlan(a, left, ti, tj, Type<T>::PLANES == 2 ? 3 : 1).splits;
   const float rest = Type<T>::PLANES == 1 ? a.rest[j] : 0.0f;
   const R* w = (const R*)a.w + (uint64_t)a.target[i] * a.ldw;
   for (uint32_t k = threadIdx.x; k < a.h; k += 256) {
@@ -668,8 +668,14 @@ __device__ __forceinline__ void dw_store(const HeadArgs& a, uint32_t c0, float f
     R* o = (R*)a.dw + (uint64_t)j * a.h + i;
     if (i + 16 <= a.h) {
       // (the hardware stores vectors at any element's address)
-      struct __attribute__((packed, aligned(sizeof(R)))) Run { R v[16]; };
-      *reinterpret_cast<Run*>(o) = __builtin_bit_cast(Run, w);
+      struct __attribute__((packed, aligned(sizeof(R)))) Run { uint32_t w[4]; } run[sizeof(w) / 16];
+      __builtin_memcpy(run, w, sizeof(w));
+#pragma unroll
+      for (uint32_t q = 0; q < sizeof(w) / 16; ++q) {
+        reinterpret_cast<Run*>(o)[q] = run[q];
+        // (else the compiler joins and splits them into pieces of 12 and 4 bytes)
+        asm volatile("" ::: "memory");
+      }
     } else {
 #pragma unroll
       for (int r = 0; r < 16; ++r)
@@ -709,6 +715,7 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, 256>::NT), 2) void k_hea
 #pragma unroll
         for (int r = 0; r < 16; ++r) v[r] = acc[x][y][r];
         if (part) {
+          if (iw + x * 32 >= a.h || jw + y * 32 >= a.v) continue;
           // as the lanes hold them: k_head_dw_tail reads them the same way
           float4* o = reinterpret_cast<float4*>(a.dw_part + ((uint64_t)mine * (G::WI * G::WJ) + y * G::WI + x) * (G::NT * 16)) + threadIdx.x * 4;
 #pragma unroll
@@ -828,7 +835,7 @@ hipError_t chunk_of(HeadArgs& a, uint32_t c0, uint32_t rows, hipStream_t st) {
     hipLaunchKernelGGL((k_head_pack<T, false>), pack, dim3(256), 0, st, a, c0, of_w);
   }
   HEAD_TRY(hipGetLastError());
-  if constexpr (!GRAD && Type<T>::PLANES == 1 && J != 128) {
+  if constexpr (!GRAD && Type<T>::PLANES == 1) {
     if (!a.wr) {
       HEAD_TRY((launch_lds<k_head_logits<T, J, false, true>>(grid_of<G>(ni * nj), G::NT, G::LDS, st, a, c0)));
     } else {
@@ -847,7 +854,7 @@ hipError_t chunk_of(HeadArgs& a, uint32_t c0, uint32_t rows, hipStream_t st) {
     HEAD_TRY(hipGetLastError());
     HEAD_TRY((launch_lds<k_head_dx<T, J>>(a.dx_grid, G::NT, G::LDS, st, a, c0)));
     if (a.n > 0) {
-      hipLaunchKernelGGL((k_head_dx_sum<T>), dim3(rows), dim3(256), 0, st, a, c0, G::TJ);
+      hipLaunchKernelGGL((k_head_dx_sum<T>), dim3(rows), dim3(256), 0, st, a, c0, G::TI, G::TJ);
       HEAD_TRY(hipGetLastError());
     }
     using W = Cfg<typename Type<T>::V8, 256>;
@@ -871,7 +878,7 @@ hipError_t head_of(HeadArgs& a, bool grad, hipStream_t st) {
   for (uint64_t c0 = 0; c0 == 0 || c0 < a.n; c0 += a.chunk) {
     const uint32_t rows = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(a.chunk, a.n - c0));
     // (one choice for every chunk: the buffers go by it)
-    const uint32_t tokens = tile_tokens(a.chunk, !a.wr), c = (uint32_t)c0;
+    const uint32_t tokens = tile_tokens(a.chunk), c = (uint32_t)c0;
     HEAD_TRY(tokens == 64    ? (grad ? chunk_of<T, 64, true>(a, c, rows, st) : chunk_of<T, 64, false>(a, c, rows, st))
              : tokens == 128 ? (grad ? chunk_of<T, 128, true>(a, c, rows, st) : chunk_of<T, 128, false>(a, c, rows, st))
                              : (grad ? chunk_of<T, 256, true>(a, c, rows, st) : chunk_of<T, 256, false>(a, c, rows, st)));
@@ -935,7 +942,8 @@ uint64_t head_plan(HeadArgs& a, int dt, bool grad, char* base) {
     a.rest = (float*)take(a.chunk * 4);
     // dx: parts of the vocabulary, as many as cost least: rounds of tiles
     // (about half a microsecond a stage) and the parts' sums written and read
-    const uint64_t tj = tile_tokens(a.chunk, false), tiles = (a.h + 255) / 256 * ((a.chunk + tj - 1) / tj);
+    const uint64_t tj = tile_tokens(a.chunk), ti = tj == 256 ? 256 : 128;
+    const uint64_t tiles = (a.h + ti - 1) / ti * ((a.chunk + tj - 1) / tj);
     const uint64_t stages = (planes == 2 ? 3 : 1) * (uint64_t)a.k_dx, room = (tj == 256 ? 1 : 2) * (uint64_t)device_cus();
     double best = 0.0;
     a.splits = 0;
