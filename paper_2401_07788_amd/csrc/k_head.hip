@@ -499,7 +499,8 @@ __global__ __launch_bounds__(256) void k_head_softmax(const HeadArgs a, uint32_t
   constexpr int PL = Type<T>::PLANES;
   using N = Numerator<T, WIDE<T, J>>;
   using R = typename N::R;
-  const uint32_t left = chunk_tokens(a, c0), j = blockIdx.y * 128u + (threadIdx.x >> 1), half = threadIdx.x & 1u;
+  // (the tokens that the logits' kernel wrote last, and the caches may hold, first)
+  const uint32_t left = chunk_tokens(a, c0), j = (gridDim.y - 1u - blockIdx.y) * 128u + (threadIdx.x >> 1), half = threadIdx.x & 1u;
   // (rows that fill the last stage of the sum over tokens are zeros)
   if (j >= (left + KSTAGE - 1) / KSTAGE * KSTAGE) return;
   const bool in = j < left;
@@ -848,7 +849,7 @@ hipError_t chunk_of(HeadArgs& a, uint32_t c0, uint32_t rows, hipStream_t st) {
                      !std::is_same_v<T, bf16_t>);
   HEAD_TRY(hipGetLastError());
   if constexpr (GRAD) {
-    const uint32_t high = (rows + 127) / 128, blocks = std::max(1u, std::min(8u, a.k_dx * high / 2048u));
+    const uint32_t high = (rows + 127) / 128, blocks = std::max(1u, std::min(4u, a.k_dx * high / 2048u));
     hipLaunchKernelGGL((k_head_softmax<T, J>), dim3((a.k_dx + blocks - 1) / blocks, high), dim3(256), 0, st, a, c0,
                        PIECE == 128 ? 7u : 6u, blocks);
     HEAD_TRY(hipGetLastError());

@@ -54,22 +54,29 @@ def _sizes(x, w, target, ignore_index, chunk):
 
 
 _ws_cache = {}
+_ws_bytes = {}          # by sizes: what a call of a shape needs
 
 
 def _workspace(c, grad: int, device, stream, ws):
     """the given workspace, else the stream's own (kept, and grown when a call needs more)"""
     if ws is not None:
-        if not ws.is_cuda or not ws.is_contiguous():
-            raise ValueError("ws must be contiguous and on the GPU")
+        if ws.device != device or not ws.is_contiguous():
+            raise ValueError(f"ws must be contiguous and on {device}")
         return ws
-    n = C.c_size_t(0)
-    tc._check(tc.lib().tc_xent_workspace_bytes(C.byref(c), grad, C.byref(n)), "tc_xent_workspace_bytes")
+    shape = (device.index, grad, c.n, c.v, c.h, c.chunk, c.dt)
+    need = _ws_bytes.get(shape)
+    if need is None:
+        n = C.c_size_t(0)
+        tc._check(tc.lib().tc_xent_workspace_bytes(C.byref(c), grad, C.byref(n)), "tc_xent_workspace_bytes")
+        if len(_ws_bytes) >= tc._PLANS_MAX:
+            _ws_bytes.clear()
+        need = _ws_bytes[shape] = n.value
     key = (device.index, stream)
     ws = _ws_cache.get(key)
-    if ws is None or ws.numel() < n.value:
+    if ws is None or ws.numel() < need:
+        del ws                      # (given back before the larger one is asked for)
         _ws_cache.pop(key, None)
-        ws = None
-        ws = _ws_cache[key] = torch.empty(max(n.value, 1 << 20), dtype=torch.uint8, device=device)
+        ws = _ws_cache[key] = torch.empty(max(need, 1 << 20), dtype=torch.uint8, device=device)
     return ws
 
 
