@@ -424,7 +424,7 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
     }
   };
   if constexpr (DIRECT) {
-    const Rows A{(const char*)a.w, a.ldw * 2, (uint32_t)a.v, nullptr};
+    const Rows A{(const char*)a.w, a.ldw * 2, (uint32_t)a.v};
     G::template stream<1>(A, B, per, lds, work, done);
   } else {
     const Blocks A{a.wr, a.v_blocks, a.wr_plane};
@@ -906,7 +906,7 @@ uint64_t head_plan(HeadArgs& a, int dt, bool grad, char* base) {
   // per token of a chunk: d, and binary32 numerators apart (16-bit ones are
   // replaced in place)
   const uint64_t per_row = grad ? (uint64_t)a.k_dx * KSTAGE * (planes == 2 ? 8 : 2) : (a.v + 63) / 64 * 8;
-  if (a.chunk == 0) a.chunk = HEAD_CHUNK_BYTES / per_row;
+  if (a.chunk == 0) a.chunk = std::min<uint64_t>(HEAD_CHUNK_BYTES / per_row, 1u << 22);
   a.chunk = std::min<uint64_t>(std::max<uint64_t>(a.chunk, 128), std::max<uint64_t>(a.n, 1));
   a.chunk = (a.chunk + 63) / 64 * 64;
   a.c_blocks = blocks(a.chunk);

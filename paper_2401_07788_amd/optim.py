@@ -6,13 +6,29 @@ libtc.so (include/tc.h), and there is no fallback."""
 from __future__ import annotations
 
 import ctypes as C
+import os
 
-import numpy as np
 import torch
 
 from . import tc
 
 BLOCK = 256     # positions of 8-bit moments that share an exponent
+
+_PY_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtc_py.so")
+_py = None
+
+
+def _addresses():
+    """tc_py_addresses of libtc_py.so (csrc/py_tensors.cpp)"""
+    global _py
+    if _py is None:
+        if not os.path.exists(_PY_PATH):
+            raise RuntimeError(f"{_PY_PATH} is missing: build it with paper_2401_07788_amd.build.build()")
+        f = C.PyDLL(_PY_PATH).tc_py_addresses
+        f.restype = C.c_int
+        f.argtypes = [C.py_object, C.c_int64, C.c_void_p, C.c_int, C.c_void_p, C.c_int64]
+        _py = f
+    return _py
 
 
 def _check_tensors(ts, what: str):
@@ -34,10 +50,11 @@ def _check_tensors(ts, what: str):
 
 class TensorList:
     """tensors of one dtype on one device, as the library takes them: a table
-    of addresses and sizes made once.  It keeps the tensors."""
+    of addresses and sizes made once.  It keeps the memory that they have now
+    (a tensor whose .data is replaced later needs a new list)."""
 
     def __init__(self, tensors):
-        self.tensors = list(tensors)
+        self.tensors = [t.detach() for t in tensors]
         self.dtype, self.device = _check_tensors(self.tensors, "tensors")
         self.table = (tc.Tensor * len(self.tensors))()
         for row, t in zip(self.table, self.tensors):
@@ -94,13 +111,31 @@ class AdamW:
         self.state = state if state is not None else self._zeros()
         self._check_state()
         self.w32 = [p.detach().float() for p in self.params] if master and self.dtype != torch.float32 else None
-        self.sizes = [p.numel() for p in self.params]
+        self.sizes = (C.c_int64 * len(self.params))(*[p.numel() for p in self.params])
         self.table = (tc.Tensor * len(self.params))()
-        # the table's column of gradient addresses, which every step fills in
-        self.g_column = np.frombuffer(self.table, dtype=np.uint64).reshape(len(self.params), -1)[:, 1]
-        for k, (row, p) in enumerate(zip(self.table, self.params)):
-            row.p, row.n, row.pos = p.data_ptr(), p.numel(), self.places[k]
+        for k, row in enumerate(self.table):
+            row.n, row.pos = self.sizes[k], self.places[k]
             row.w32 = self.w32[k].data_ptr() if self.w32 else None
+
+    def _fill(self, tensors, column: int):
+        """the tensors' addresses into the table (0: p, 1: g); their dtype as
+        the library numbers it, or -1 where they are not what they must be"""
+        return _addresses()(tensors, len(self.table), self.sizes, self.device.index, C.addressof(self.table) + 8 * column,
+                            C.sizeof(tc.Tensor) // 8)
+
+    def _refuse(self, grads):
+        """what is wrong with the tensors of a step"""
+        if len(grads) != len(self.params):
+            raise ValueError(f"{len(grads)} gradients for {len(self.params)} parameters")
+        if any(g is None for g in grads):
+            raise ValueError("a parameter has no gradient")
+        _, device = _check_tensors(grads, "gradients")
+        if device != self.device:
+            raise ValueError(f"gradients must be on {self.device}")
+        if [g.numel() for g in grads] != list(self.sizes):
+            raise ValueError("a gradient does not fit its parameter")
+        tc._need_gpu(*grads, *self.params)
+        raise ValueError("a parameter changed its dtype, device or size")
 
     def _spec(self):
         if self.bits == 32:
@@ -125,28 +160,21 @@ class AdamW:
         Where the norm is not finite nothing is changed but the step count."""
         if grads is None:
             grads = [p.grad for p in self.params]
-        if len(grads) != len(self.params):
-            raise ValueError(f"{len(grads)} gradients for {len(self.params)} parameters")
-        # (every call's tensors are looked at; one pass per property is the cheapest way)
-        gdt, dev = grads[0].dtype, self.device
-        at = -1 if dev.index is None else dev.index
-        if [g.get_device() for g in grads] != [at] * len(grads) or {g.dtype for g in grads} != {gdt}:
-            raise TypeError(f"gradients must be of one dtype on {dev}")
-        if [g.numel() for g in grads] != self.sizes or not all([g.is_contiguous() for g in grads]):
-            raise ValueError("a gradient does not fit its parameter, or is not contiguous")
-        if gdt not in tc._DT:
-            raise TypeError(f"unsupported dtype {gdt}")
-        self.g_column[:] = [g.data_ptr() for g in grads]
+        grads, dev = list(grads), self.device
         if clip is not None and (clip.dtype != torch.float32 or clip.numel() != 2 or clip.device != dev or
                                  not clip.is_contiguous()):
             raise ValueError(f"clip must be float32 [2] on {dev}")
-        tc._need_gpu(self.params[0])
+        gdt = self._fill(grads, 1) if dev.type == "cuda" else -1
+        if gdt < 0 or self._fill(self.params, 0) != tc._DT[self.dtype]:
+            self._refuse(grads)
         st = self.state
+        if st["m"].numel() != self.size or st["v"].numel() != self.size:
+            self._check_state()
         t = self.t + 1
         a = tc.AdamwSettings(self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay, t, self.bits,
                              (self.seed + 1) & 0x7FFFFFFF, st["m"].data_ptr(), st["v"].data_ptr(),
                              tc._ptr(st.get("em")), tc._ptr(st.get("ev")))
-        tc._check(tc.lib().tc_adamw_step(C.byref(a), self.table, len(self.table), tc._DT[self.dtype], tc._DT[gdt],
+        tc._check(tc.lib().tc_adamw_step(C.byref(a), self.table, len(self.table), tc._DT[self.dtype], gdt,
                                          tc._ptr(clip), tc._stream(dev)), "tc_adamw_step")
         self.t, self.seed = t, (self.seed + 1) & 0x7FFFFFFF
 
@@ -156,7 +184,8 @@ class AdamW:
         st = self.state
         if self.bits == 32:
             return st["m"], st["v"]
-        m, v = torch.empty((2, self.size), dtype=torch.float32, device=self.device)
+        m = torch.empty(self.size, dtype=torch.float32, device=self.device)
+        v = torch.empty(self.size, dtype=torch.float32, device=self.device)
         tc._need_gpu(m)
         tc._check(tc.lib().tc_adamw_moments(st["m"].data_ptr(), st["em"].data_ptr(), st["v"].data_ptr(),
                                             st["ev"].data_ptr(), self.size, m.data_ptr(), v.data_ptr(),

@@ -245,3 +245,20 @@ def test_step_takes_grad_attributes_and_other_streams(optim):
     side.synchronize()
     b.step([p.grad])
     assert torch.equal(p.data, q)
+
+
+def test_parameters_whose_data_was_replaced(optim):
+    """the step goes to the memory that they have now"""
+    ps = [torch.nn.Parameter(torch.randn(300, device="cuda")), torch.nn.Parameter(torch.randn(70, device="cuda"))]
+    opt = optim.AdamW(ps, **HP)
+    gs = [torch.randn_like(p) for p in ps]
+    opt.step(gs)
+    old = ps[1].data
+    kept = old.clone()
+    ps[1].data = old.clone()
+    opt.step(gs)
+    assert torch.equal(old, kept) and not torch.equal(ps[1].data, kept)
+    ps[1].data = torch.zeros(71, device="cuda")
+    with pytest.raises(ValueError, match="changed"):
+        opt.step([gs[0], torch.zeros(70, device="cuda")])
+    assert opt.t == 2
