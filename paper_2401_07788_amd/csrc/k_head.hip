@@ -180,11 +180,12 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v) {
 }
 
 // The list as the other kernels read it, zero losses for the others, and the
-// largest weight.
-template <int NT>
-__device__ __forceinline__ uint32_t write_rows(const HeadArgs& a) {
+// largest weight.  also(i, keep, at) is called as list_rows would.
+template <int NT, typename Also>
+__device__ __forceinline__ uint32_t write_rows(const HeadArgs& a, Also also) {
   uint32_t top = 0;
   const uint32_t kept = list_rows<NT>(a, [&](uint32_t i, bool keep, uint32_t at) {
+    also(i, keep, at);
     a.rows[at] = i;
     if (keep) {
       top = max(top, a.weight ? __float_as_uint(a.weight[i]) & 0x7FFFFFFFu : 0x3F800000u);
@@ -208,7 +209,7 @@ constexpr int BNT = 1024;
 
 __global__ __launch_bounds__(BNT) void k_head_begin(const HeadArgs a) {
   if (blockIdx.x == 0) {
-    write_rows<BNT>(a);
+    write_rows<BNT>(a, [](uint32_t, bool, uint32_t) {});
     return;
   }
   const uint32_t b = blockIdx.x - 1u, lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
@@ -298,10 +299,10 @@ __global__ __launch_bounds__(256) void k_head_pack(const HeadArgs a, uint32_t c0
   }
   uint32_t rows;
   if constexpr (ALONE) {
-    if (b == 0) write_rows<256>(a);
-    rows = list_rows<256>(a, [&](uint32_t i, bool keep, uint32_t at) {
+    auto mine = [&](uint32_t i, bool keep, uint32_t at) {
       if (keep && at >> 4 == rb) list[at & 15u] = i;
-    });
+    };
+    rows = b == 0 ? write_rows<256>(a, mine) : list_rows<256>(a, mine);
   } else {
     rows = chunk_tokens(a, c0);
     if (threadIdx.x < 16 && rb * 16u + threadIdx.x < rows) list[threadIdx.x] = a.rows[c0 + rb * 16u + threadIdx.x];
