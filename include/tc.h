@@ -348,8 +348,9 @@ tc_status tc_xent_workspace_bytes(const tc_xent* c, int grad, size_t* bytes);
 /* loss[i] = lse[i] - z[target[i]] and lse[i] = log sum_v exp z[v] with
  * z[v] = sum_k x[i][k] w[v][k], products and sums in binary32 (binary32 inputs
  * are multiplied as pairs of binary16 values: 22 bits of an element down to
- * 2^-28 of the largest magnitude of its matrix).  loss, lse: [n] binary32;
- * target: [n] on the device. */
+ * 2^-28 of the largest finite magnitude of its matrix; a logit that an infinity
+ * takes part in is an infinity or NaN).  A logit of -inf is an entry with
+ * probability 0.  loss, lse: [n] binary32; target: [n] on the device. */
 tc_status tc_xent_loss(const tc_xent* c, const void* x, const void* w, const int64_t* target, float* loss, float* lse,
                        void* ws, size_t ws_bytes, void* stream);
 

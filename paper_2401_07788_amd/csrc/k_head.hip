@@ -9,7 +9,7 @@
 // length stays on the device (tiles past it end at once).
 //
 // The loss needs one product.  Its epilogue reduces each token's logits, a
-// piece of 64 or 128 vocabulary entries at a time, to their maximum and the
+// piece of 64 vocabulary entries at a time, to their maximum and the
 // sum of their exponentials; a small kernel joins the pieces.  With gradients
 // the epilogue also leaves exp(z - piece's maximum), 16 bits each, so that the
 // logits are computed once (6 n v h operations, not 8); another pass turns
@@ -91,6 +91,13 @@ struct Info {
 __device__ __forceinline__ uint32_t chunk_tokens(const HeadArgs& a, uint32_t c0) {
   const uint32_t n = ((const Info*)a.info)->count;
   return min(n > c0 ? n - c0 : 0u, (uint32_t)a.chunk);
+}
+
+// The pattern of a magnitude for such a maximum.  Infinities and NaN stay out:
+// they spoil what they take part in, and a scaling by them would all the rest.
+__device__ __forceinline__ uint32_t magnitude(float v) {
+  const uint32_t m = __float_as_uint(v) & 0x7FFFFFFFu;
+  return m < 0x7F800000u ? m : 0u;
 }
 
 // exponent that scales a binary32 operand: the largest magnitude becomes 2^14 .. 2^15
@@ -188,7 +195,7 @@ __device__ __forceinline__ uint32_t write_rows(const HeadArgs& a, Also also) {
     also(i, keep, at);
     a.rows[at] = i;
     if (keep) {
-      top = max(top, a.weight ? __float_as_uint(a.weight[i]) & 0x7FFFFFFFu : 0x3F800000u);
+      top = max(top, a.weight ? magnitude(a.weight[i]) : 0x3F800000u);
     } else {
       a.loss[i] = a.lse[i] = 0.0f;
       if (a.target[i] != a.ignore) raise_error(KERR_BAD_INDEX);
@@ -215,12 +222,16 @@ __global__ __launch_bounds__(BNT) void k_head_begin(const HeadArgs a) {
   const uint32_t b = blockIdx.x - 1u, lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
   const bool of_w = b >= a.top_x;
   const uint64_t rows = of_w ? a.v : a.n, first = of_w ? b - a.top_x : b, step = (of_w ? a.top_w : a.top_x) * (uint64_t)(BNT / WAVE);
+  // (a wavefront takes several short rows at a time)
+  uint32_t wide = 64;
+  while (wide > 1 && wide / 2 >= a.h) wide /= 2;
+  const uint32_t at_once = 64 / wide;
   uint32_t top = 0;
-  for (uint64_t r = first * (BNT / WAVE) + wave; r < rows; r += step) {
+  for (uint64_t r = (first * (BNT / WAVE) + wave) * at_once + lane / wide; r < rows; r += step * at_once) {
     if (!of_w && !has_target(a, a.target[r])) continue;
     const float* p = of_w ? (const float*)a.w + r * a.ldw : (const float*)a.x + r * a.ldx;
 #pragma unroll 8
-    for (uint32_t k = lane; k < a.h; k += 64) top = max(top, __float_as_uint(p[k]) & 0x7FFFFFFFu);
+    for (uint32_t k = lane & (wide - 1); k < a.h; k += wide) top = max(top, magnitude(p[k]));
   }
   top = block_max<BNT>(top);
   if (threadIdx.x == 0) a.tops[b] = top;
@@ -261,7 +272,7 @@ __device__ __forceinline__ void pack_rows(const HeadArgs& a, uint32_t rows, cons
       for (int z = 0; z < 8; ++z) {
         const float s = __builtin_ldexpf(v.v[z], e);
         hi[z] = Elem<f16_t>::down(s);
-        lo[z] = Elem<f16_t>::down(s - Elem<f16_t>::up(hi[z]));
+        lo[z] = (hi[z] & 0x7FFFu) == 0x7C00u ? (uint16_t)0 : Elem<f16_t>::down(s - Elem<f16_t>::up(hi[z]));
       }
       __builtin_memcpy(o, hi, 16);
       __builtin_memcpy(o + (OF_W ? a.wr_plane : a.xr_plane), lo, 16);
@@ -392,7 +403,8 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
       }
       // one rounding of top * log2 e is common to the piece: it moves its part of lse by 2^-24 of top
       float sum = 0.0f;
-      const float shift = -top * LOG2E;
+      // (a piece of logits that are all -inf adds nothing)
+      const float shift = top > -__builtin_inff() ? -top * LOG2E : 0.0f;
 #pragma unroll
       for (int x = 0; x < G::WI; ++x) {
 #pragma unroll
@@ -456,12 +468,11 @@ __global__ __launch_bounds__(SNT) void k_head_loss(const HeadArgs a, uint32_t c0
       }
 #pragma unroll
       for (uint32_t k = 0; k < B; ++k) top = fmaxf(top, v[k].x);
-      // (pieces whose logits are all -inf add nothing)
-      if (top > -__builtin_inff()) {
-        s *= __expf(m - top);
+      // (where all logits are -inf so far the sums are 0, or NaN where one is)
+      const bool any = top > -__builtin_inff();
+      s *= any ? __expf(m - top) : 1.0f;
 #pragma unroll
-        for (uint32_t k = 0; k < B; ++k) s += v[k].y * __expf(v[k].x - top);
-      }
+      for (uint32_t k = 0; k < B; ++k) s = __builtin_fmaf(v[k].y, any ? __expf(v[k].x - top) : 1.0f, s);
       m = top;
     }
   }
@@ -485,7 +496,7 @@ __global__ __launch_bounds__(SNT) void k_head_loss(const HeadArgs a, uint32_t c0
     a.loss[i] = lse - a.zt[jj];
     if (a.row_info) {
       const float g = a.weight ? a.weight[i] : 1.0f, most = __uint_as_float(((const Info*)a.info)->top_g);
-      const float weight = !share ? g : most > 0.0f ? g / most : 0.0f;
+      const float weight = !share ? g : most > 0.0f ? g / most : g;
       a.row_info[jj] = make_float4(lse, weight, __uint_as_float((uint32_t)a.target[i]), 0.0f);
     }
   }

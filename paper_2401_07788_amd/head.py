@@ -71,10 +71,13 @@ def _workspace(c, grad: int, device, stream, ws):
         if len(_ws_bytes) >= tc._PLANS_MAX:
             _ws_bytes.clear()
         need = _ws_bytes[shape] = n.value
+    if torch.cuda.is_current_stream_capturing():
+        # a graph keeps its own: a larger call would free the stream's under it
+        return torch.empty(need, dtype=torch.uint8, device=device)
     key = (device.index, stream)
     ws = _ws_cache.get(key)
     if ws is None or ws.numel() < need:
-        del ws                      # (given back before the larger one is asked for)
+        ws = None                   # (given back before the larger one is asked for)
         _ws_cache.pop(key, None)
         ws = _ws_cache[key] = torch.empty(max(need, 1 << 20), dtype=torch.uint8, device=device)
     return ws

@@ -72,6 +72,9 @@ def grad_norm(grads, max_norm: float, out: torch.Tensor = None, ws: torch.Tensor
     elif out.dtype != torch.float32 or out.numel() != 2 or out.device != lst.device:
         raise ValueError(f"out must be float32 [2] on {lst.device}")
     st = tc._stream(lst.device)
+    if ws is None and torch.cuda.is_current_stream_capturing():
+        # a graph keeps its own: a larger call would free the stream's under it
+        ws = torch.zeros(lst.ws_bytes, dtype=torch.uint8, device=lst.device)
     if ws is None:
         ws = tc._ws_cache.get((lst.device.index, st))
         if ws is None or ws.numel() < lst.ws_bytes:

@@ -271,3 +271,94 @@ def test_replays_in_a_graph(head):
         torch.cuda.synchronize()
         for p, q in zip(out, want):
             assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("first,count", [(0, 64), (64, 130), (190, 110), (3, 296)])
+def test_logits_of_minus_infinity(head, dt, first, count):
+    """entries that a row of w takes out: whole pieces of them, and all but a few"""
+    n, v, h = 70, 300, 64
+    x, w, t = inputs(n, v, h, dt, 14)
+    x[:, 0] = 1.0
+    out = torch.zeros(v, dtype=torch.bool, device="cuda")
+    out[first:first + count] = True
+    w[out] = 0.0
+    w[out, 0] = -math.inf
+    keep = (~out).nonzero()[:, 0]
+    t = keep[t % len(keep)]
+    r = head.linear_xent_step(x, w, t)
+    place = torch.full((v,), -1, device="cuda")
+    place[keep] = torch.arange(len(keep), device="cuda")
+    dense = type("R", (), {"loss": r.loss, "lse": r.lse})()
+    check(dense, x, w[keep], place[t], None, dt, len(keep))
+    loss, lse = head.linear_xent(x, w, t)
+    assert torch.equal(loss, r.loss) and torch.equal(lse, r.lse)
+    # (dx holds 0 times -inf in every definition)
+    want, size = reference(x, w[keep], place[t], None, len(keep))
+    rel = UD[dt] + 2.0 ** -10
+    assert not r.dw[out].any()
+    lim = rel * size["dw"] + U[dt] * want["dw"].abs() + (2.0 ** -24 if dt == "f16" else 1e-38) + 2.0 ** -37 * size["x"]
+    assert bool(((r.dw[keep].double().cpu() - want["dw"]).abs() <= lim).all())
+
+
+@pytest.mark.parametrize("dt", list(DT))
+def test_nan_entries_reach_every_loss(head, dt):
+    n, v, h = 40, 300, 64
+    x, w, t = inputs(n, v, h, dt, 15)
+    w[128:192] = math.nan
+    assert torch.isnan(head.linear_xent(x, w, t)[0]).all()
+    assert torch.isnan(head.linear_xent_step(x, w, t).loss).all()
+
+
+@pytest.mark.parametrize("dt", list(DT))
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+def test_a_token_that_is_not_finite_spoils_no_other(head, dt, bad):
+    n, v, h = 140, 300, 64
+    x, w, t = inputs(n, v, h, dt, 16)
+    weight = torch.rand(n, device="cuda") + 0.5
+    others = torch.ones(n, dtype=torch.bool, device="cuda")
+    others[33] = False
+    for into_x in (True, False):
+        x2, weight2 = x.clone(), weight.clone()
+        if into_x:
+            x2[33, 5] = bad
+        else:
+            weight2[33] = bad
+        r = head.linear_xent_step(x2, w, t, weight2)
+        assert torch.isnan(r.loss[33]) == into_x and not torch.isfinite(r.dx[33]).all()
+        assert torch.isfinite(r.dx[others]).all() and torch.isfinite(r.loss[others]).all()
+        part = type("R", (), {"loss": r.loss[others], "lse": r.lse[others]})()
+        check(part, x[others], w, t[others], weight[others], dt, v)
+        want, size = reference(x[others], w, t[others], weight[others], v)
+        rel = UD[dt] + 2.0 ** -10
+        lim = rel * size["dx"] + U[dt] * want["dx"].abs() + (2.0 ** -24 if dt == "f16" else 1e-38) + \
+            2.0 ** -36 * w.double().cpu().abs().sum(0)
+        assert bool(((r.dx[others].double().cpu() - want["dx"]).abs() <= lim).all())
+
+
+def test_a_graph_has_a_workspace_of_its_own(head):
+    """a larger call on the same stream between the replays does not reach it"""
+    x, w, t = inputs(150, 600, 64, "bf16", 17)
+    want = head.linear_xent_step(x, w, t)
+    out = head.XentStep(*[torch.empty_like(p) for p in want])
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        head.linear_xent_step(x, w, t)
+    side.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        head.linear_xent_step(x, w, t, out=out)
+    big = inputs(1000, 5000, 64, "bf16", 18)
+    for _ in range(3):
+        for p in out:
+            p.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            head.linear_xent_step(*big)
+            filler = torch.full((64 << 20,), 255, dtype=torch.uint8, device="cuda")
+        side.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        del filler
+        for p, q in zip(out, want):
+            assert torch.equal(p, q)
