@@ -137,6 +137,7 @@ class _LinearXent(torch.autograd.Function):
         return loss, lse
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, g, _):
         x, w, target = ctx.saved_tensors
         r = linear_xent_step(x, w, target, g.to(torch.float32).contiguous(), *ctx.more)
@@ -145,7 +146,7 @@ class _LinearXent(torch.autograd.Function):
 
 def linear_xent(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, ignore_index: int = -100, chunk: int = 0):
     """(loss, lse), float32 [n]: the losses of the tokens x [n, h] against
-    w [v, h].  The losses are differentiable in x and w; lse is not."""
+    w [v, h].  The losses are differentiable in x and w, once; lse is not."""
     if torch.is_grad_enabled() and (x.requires_grad or w.requires_grad):
         return _LinearXent.apply(x, w, target, ignore_index, chunk)
     return _loss(x, w, target, ignore_index, chunk)

@@ -362,3 +362,13 @@ def test_a_graph_has_a_workspace_of_its_own(head):
         del filler
         for p, q in zip(out, want):
             assert torch.equal(p, q)
+
+
+def test_the_gradients_are_not_differentiable(head):
+    """a second derivative is refused, not taken for zero"""
+    x, w, t = inputs(20, 30, 16, "f32", 19)
+    x, w = x.contiguous().requires_grad_(), w.contiguous().requires_grad_()
+    loss, _ = head.linear_xent(x, w, t)
+    dx, = torch.autograd.grad(loss.sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        dx.square().sum().backward()
