@@ -160,13 +160,16 @@ class AdamW:
     def step(self, grads=None, clip: torch.Tensor = None):
         """one step.  grads: a tensor per parameter (of one dtype), else their
         .grad; clip: what grad_norm returned, else the gradients as they are.
-        Where the norm is not finite nothing is changed but the step count."""
+        Where the norm is not finite nothing is changed but the step count.
+        Not for a graph: the step's number and seed are part of the call."""
         if grads is None:
             grads = [p.grad for p in self.params]
         grads, dev = list(grads), self.device
         if clip is not None and (clip.dtype != torch.float32 or clip.numel() != 2 or clip.device != dev or
                                  not clip.is_contiguous()):
             raise ValueError(f"clip must be float32 [2] on {dev}")
+        if dev.type == "cuda" and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("a captured step would repeat its number and seed at every replay")
         gdt = self._fill(grads, 1) if dev.type == "cuda" else -1
         if gdt < 0 or self._fill(self.params, 0) != tc._DT[self.dtype]:
             self._refuse(grads)

@@ -262,3 +262,20 @@ def test_parameters_whose_data_was_replaced(optim):
     with pytest.raises(ValueError, match="changed"):
         opt.step([gs[0], torch.zeros(70, device="cuda")])
     assert opt.t == 2
+
+
+def test_a_step_is_not_captured(optim):
+    """its number and seed would be the same at every replay"""
+    ps, _, _ = views([300], torch.float32, 0, 30)
+    gs, _, _ = views([300], torch.float32, 0, 31)
+    opt, other = optim.AdamW(ps, state_bits=8, **HP), torch.ones(4, device="cuda")
+    torch.cuda.synchronize()
+    before = ps[0].clone()
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        other.zero_()
+        with pytest.raises(RuntimeError, match="captured"):
+            opt.step(gs)
+    torch.cuda.synchronize()
+    assert opt.t == 0 and torch.equal(ps[0], before)
+    opt.step(gs)
+    assert opt.t == 1 and not torch.equal(ps[0], before)
