@@ -215,7 +215,7 @@ struct Gemm {
   // returns false, done(n, w, acc) takes its sums.  The stages of all of them
   // are one stream: while the last ones of a piece are multiplied, the first
   // ones of the next are loaded, and they land while done() runs (which
-  // therefore has no LDS).
+  // therefore has the LDS past the slots only).
   template <int PAIRS, typename OA, typename OB, typename WorkOf, typename Done>
   static __device__ __forceinline__ void stream(const OA& A, const OB& B, uint32_t per, char* lds, WorkOf work, Done done) {
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
