@@ -652,9 +652,9 @@ __global__ __launch_bounds__(256) void k_head_dx_sum(const HeadArgs a, uint32_t 
 // tokens, so that it takes a part of a round, and joined by k_head_dw_tail.
 // One chunk: rounded to its dtype here.  More: binary32 sums from chunk to
 // chunk, rounded by k_head_dw_round after the last.
-template <typename T>
+template <typename T, int W>
 struct DwPlan {
-  using G = Cfg<typename Type<T>::V8, 256>;
+  using G = Cfg<typename Type<T>::V8, W>;
   uint32_t ni, nj, whole, rest, all, parts;
   __device__ __forceinline__ DwPlan(const HeadArgs& a, uint32_t left) {
     ni = (a.h + G::TI - 1) / G::TI;
@@ -721,16 +721,23 @@ constexpr uint32_t RUN_LDS = 4096;       // of a wavefront: 16 rows of 256 bytes
 template <typename T, int WI, int WJ>
 __device__ __forceinline__ void dw_store_runs(const HeadArgs& a, float f, char* lds, uint32_t lane, uint32_t i0, uint32_t j0, f32x16 (&acc)[WI][WJ]) {
   using R = typename Elem<T>::raw;
-  constexpr uint32_t E = sizeof(R), RUN = 256 / E, XF = RUN / 32, Q = E, PER = 16 / E;   // Q pieces of PER elements a fragment row
+  // XF fragments side by side make a run (128 bytes where a wavefront has no
+  // more), Q pieces of PER elements to a lane's row of each
+  constexpr uint32_t E = sizeof(R), XF = 8 / E < WI ? 8 / E : WI, RUN = XF * 32, Q = E, PER = 16 / E;
+  constexpr uint32_t PIECES = RUN / PER, READ_ROWS = 64 / PIECES, READS = 16 / READ_ROWS;
+  static_assert(WI % XF == 0 && (READS == 2 || READS == 4), "whole runs");
   struct __attribute__((packed, aligned(sizeof(R)))) Run { u32x4 w; };
   struct __attribute__((packed, aligned(sizeof(R)))) Run8 { uint32_t w[2]; };
   struct __attribute__((packed, aligned(sizeof(R)))) Run4 { uint32_t w; };
-  const uint32_t h = lane >> 5, r = lane & 15u, p = lane & 15u, group = lane >> 4;
+  const uint32_t h = lane >> 5, r = lane & 15u, p = lane % PIECES, group = lane / PIECES;
   const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-  const uint32_t to = at + r * 256u;
-  uint32_t from[4];
+  const uint32_t to = at + r * RUN * E;
+  uint32_t from[READS];
 #pragma unroll
-  for (uint32_t q = 0; q < 4; ++q) from[q] = at + (q * 4u + group) * 256u + (p ^ (q * 4u + group)) * 16u;
+  for (uint32_t q = 0; q < READS; ++q) {
+    const uint32_t row = q * READ_ROWS + group;
+    from[q] = at + (row * PIECES + (p ^ (row % PIECES))) * 16u;
+  }
 #pragma unroll
   for (int y = 0; y < WJ; ++y)
 #pragma unroll
@@ -752,19 +759,25 @@ __device__ __forceinline__ void dw_store_runs(const HeadArgs& a, float f, char* 
           for (uint32_t x = 0; x < XF; ++x)
 #pragma unroll
             for (uint32_t q = 0; q < Q; ++q)
-              asm volatile("ds_write_b128 %0, %1" ::"v"(to + (((x * 2u + h) * Q + q) ^ r) * 16u), "v"(v[x][q]) : "memory");
+              asm volatile("ds_write_b128 %0, %1" ::"v"(to + (((x * 2u + h) * Q + q) ^ (r % PIECES)) * 16u), "v"(v[x][q]) : "memory");
         }
         __builtin_amdgcn_sched_barrier(0);
-        u32x4 o[4];
-        asm volatile("s_waitcnt lgkmcnt(0)\n\tds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\t"
-                     "ds_read_b128 %3, %7\n\ts_waitcnt lgkmcnt(0)"
-                     : "=&v"(o[0]), "=&v"(o[1]), "=&v"(o[2]), "=&v"(o[3])
-                     : "v"(from[0]), "v"(from[1]), "v"(from[2]), "v"(from[3])
-                     : "memory");
+        u32x4 o[READS];
+        if constexpr (READS == 4)
+          asm volatile("s_waitcnt lgkmcnt(0)\n\tds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\t"
+                       "ds_read_b128 %3, %7\n\ts_waitcnt lgkmcnt(0)"
+                       : "=&v"(o[0]), "=&v"(o[1]), "=&v"(o[2]), "=&v"(o[3])
+                       : "v"(from[0]), "v"(from[1]), "v"(from[2]), "v"(from[3])
+                       : "memory");
+        else
+          asm volatile("s_waitcnt lgkmcnt(0)\n\tds_read_b128 %0, %2\n\tds_read_b128 %1, %3\n\ts_waitcnt lgkmcnt(0)"
+                       : "=&v"(o[0]), "=&v"(o[1])
+                       : "v"(from[0]), "v"(from[1])
+                       : "memory");
         const uint32_t i = i0 + g * RUN + p * PER;
 #pragma unroll
-        for (uint32_t q = 0; q < 4; ++q) {
-          const uint32_t j = j0 + y * 32u + s * 16u + q * 4u + group;
+        for (uint32_t q = 0; q < READS; ++q) {
+          const uint32_t j = j0 + y * 32u + s * 16u + q * READ_ROWS + group;
           if (j >= a.v || i >= a.h) continue;
           R* d = (R*)a.dw + (uint64_t)j * a.h + i;
           // (the hardware stores vectors at any element's address)
@@ -800,13 +813,13 @@ __device__ __forceinline__ float dw_factor(const HeadArgs& a) {
   return f;
 }
 
-template <typename T>
-__global__ __launch_bounds__((Cfg<typename Type<T>::V8, 256>::NT), 2) void k_head_dw(const HeadArgs a, uint32_t c0) {
-  using G = Cfg<typename Type<T>::V8, 256>;
+template <typename T, int W>
+__global__ __launch_bounds__((Cfg<typename Type<T>::V8, W>::NT), 2) void k_head_dw(const HeadArgs a, uint32_t c0) {
+  using G = Cfg<typename Type<T>::V8, W>;
   extern __shared__ __attribute__((aligned(128))) char lds[];
   const uint32_t left = chunk_tokens(a, c0);
   if (c0 > 0 && left == 0) return;
-  const DwPlan<T> plan(a, left);
+  const DwPlan<T, W> plan(a, left);
   const float f = dw_factor<T>(a);
   const uint32_t mine = die_tile(blockIdx.x, gridDim.x);
   auto done = [&](uint32_t n, const typename G::Work& at, f32x16 (&acc)[G::WI][G::WJ]) {
@@ -865,12 +878,12 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, 256>::NT), 2) void k_hea
 }
 
 // one fragment row of a tile of the last round per workgroup
-template <typename T>
-__global__ __launch_bounds__((Cfg<typename Type<T>::V8, 256>::NT)) void k_head_dw_tail(const HeadArgs a, uint32_t c0) {
-  using G = Cfg<typename Type<T>::V8, 256>;
+template <typename T, int W>
+__global__ __launch_bounds__((Cfg<typename Type<T>::V8, W>::NT)) void k_head_dw_tail(const HeadArgs a, uint32_t c0) {
+  using G = Cfg<typename Type<T>::V8, W>;
   const uint32_t left = chunk_tokens(a, c0);
   if (left == 0) return;
-  const DwPlan<T> plan(a, left);
+  const DwPlan<T, W> plan(a, left);
   const uint32_t tile = blockIdx.x / (G::WI * G::WJ), xy = blockIdx.x % (G::WI * G::WJ), x = xy % G::WI, y = xy / G::WI;
   float v[16] = {};
   for (uint32_t p = 0; p < plan.parts; ++p) {
@@ -931,6 +944,18 @@ uint32_t grid_of(uint64_t tiles) {
 template <typename T>
 bool alone(const HeadArgs& a) { return Type<T>::PLANES == 1 && a.n <= ALONE_TOKENS && a.n <= a.chunk; }
 
+template <typename T, int W>
+hipError_t launch_dw(const HeadArgs& a, uint32_t c0, hipStream_t st) {
+  using G = Cfg<typename Type<T>::V8, W>;
+  HEAD_TRY((launch_lds<k_head_dw<T, W>>(a.dw_grid, G::NT, G::LDS + G::NW * RUN_LDS, st, a, c0)));
+  if (a.dw_parts) {
+    const uint32_t tiles = ((a.h + G::TI - 1) / G::TI) * (((uint32_t)a.v + G::TJ - 1) / G::TJ);
+    hipLaunchKernelGGL((k_head_dw_tail<T, W>), dim3(tiles % a.dw_grid * (G::WI * G::WJ)), dim3(G::NT), 0, st, a, c0);
+    HEAD_TRY(hipGetLastError());
+  }
+  return hipSuccess;
+}
+
 template <typename T, int J, bool GRAD>
 hipError_t chunk_of(HeadArgs& a, uint32_t c0, uint32_t rows, hipStream_t st) {
   using G = Cfg<typename Type<T>::V8, J>;
@@ -968,13 +993,7 @@ hipError_t chunk_of(HeadArgs& a, uint32_t c0, uint32_t rows, hipStream_t st) {
       hipLaunchKernelGGL((k_head_dx_sum<T>), dim3(rows), dim3(256), 0, st, a, c0, G::TI, G::TJ);
       HEAD_TRY(hipGetLastError());
     }
-    using W = Cfg<typename Type<T>::V8, 256>;
-    HEAD_TRY((launch_lds<k_head_dw<T>>(a.dw_grid, W::NT, W::LDS + W::NW * RUN_LDS, st, a, c0)));
-    if (a.dw_parts) {
-      const uint32_t tiles = ((a.h + W::TI - 1) / W::TI) * (((uint32_t)a.v + W::TJ - 1) / W::TJ);
-      hipLaunchKernelGGL((k_head_dw_tail<T>), dim3(tiles % a.dw_grid * (W::WI * W::WJ)), dim3(W::NT), 0, st, a, c0);
-      HEAD_TRY(hipGetLastError());
-    }
+    HEAD_TRY((a.dw_small ? launch_dw<T, 64>(a, c0, st) : launch_dw<T, 256>(a, c0, st)));
   }
   return hipSuccess;
 }
@@ -1068,12 +1087,29 @@ uint64_t head_plan(HeadArgs& a, int dt, bool grad, char* base) {
     }
     a.dx_part = (float*)take(a.splits * a.chunk * a.hq * 4);
     a.dx_grid = (uint32_t)((std::min(room, tiles * std::max<uint64_t>(stages / 16, 1)) + 7) / 8 * 8);
-    // dw: the tiles past the last whole round in as many parts as fill one
-    const uint64_t wt = (a.h + 255) / 256 * ((a.v + 255) / 256), cus = (uint64_t)(device_cus() + 7) / 8 * 8;
-    a.dw_grid = (uint32_t)std::min<uint64_t>(cus, (wt + 7) / 8 * 8);
-    const uint64_t rest = wt % a.dw_grid;
-    a.dw_parts = rest && a.dw_grid >= 2 * rest ? (uint32_t)std::min<uint64_t>(a.dw_grid / rest, 16) : 0;
-    a.dw_part = (float*)take(rest * a.dw_parts * 256 * 256 * 4);
+    // dw: 256 x 256 tiles, or 128 x 64 where those would leave two thirds of
+    // the compute units idle (4096 tokens, 4000 entries, h 1024, 64 tiles: the
+    // step in 189 us, not 220; 61 x 1009 x 97 in binary32: 41.5, not 44.4)
+    const uint64_t cus = (uint64_t)(device_cus() + 7) / 8 * 8;
+    a.dw_small = (a.h + 255) / 256 * ((a.v + 255) / 256) * 3 <= cus;
+    const uint64_t wi = a.dw_small ? 128 : 256, wj = a.dw_small ? 64 : 256, slots = a.dw_small ? 2 * cus : cus;
+    const uint64_t wt = (a.h + wi - 1) / wi * ((a.v + wj - 1) / wj), rows = (planes == 2 ? 3 : 1) * ((a.chunk + KSTAGE - 1) / KSTAGE);
+    a.dw_grid = (uint32_t)std::min<uint64_t>(slots, (wt + 7) / 8 * 8);
+    a.dw_parts = 0;
+    if (wt < slots) {
+      // less than a round: in parts of 16 stages at least, where that makes it a
+      // third as long (4096 x 1009 x 97 in binary32: the step 178 -> 93 us; two
+      // parts gain nothing on the kernel that joins them)
+      const uint64_t parts = std::min<uint64_t>(std::min<uint64_t>(slots / wt, rows / 16), 16);
+      if (parts >= 3) {
+        a.dw_parts = (uint32_t)parts;
+        a.dw_grid = (uint32_t)((wt * parts + 7) / 8 * 8);
+      }
+    } else if (const uint64_t rest = wt % a.dw_grid; rest && a.dw_grid >= 2 * rest) {
+      // the tiles past the last whole round in as many parts as fill one
+      a.dw_parts = (uint32_t)std::min<uint64_t>(a.dw_grid / rest, 16);
+    }
+    a.dw_part = (float*)take(wt % a.dw_grid * a.dw_parts * wi * wj * 4);
     a.dw_sum = one ? nullptr : (float*)take(a.v * a.hq * 4);
   }
   return at;

@@ -194,7 +194,8 @@ struct HeadArgs {
   float* dx_part;        // [splits][chunk][hq]
   float* dw_sum;         // [v][hq], or nullptr with one chunk
   uint32_t dw_grid, dw_parts;   // workgroups of dw's product; parts of its last round's tiles
-  float* dw_part;        // [tiles of the last round][dw_parts][256 * 256]
+  bool dw_small;                // 128 x 64 tiles, not 256 x 256
+  float* dw_part;        // [tiles of the last round][dw_parts][a tile]
 };
 // bytes that the per-token buffers of a chunk may take unless the caller chooses
 constexpr uint64_t HEAD_CHUNK_BYTES = 4ull << 30;

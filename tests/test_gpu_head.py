@@ -372,3 +372,11 @@ def test_the_gradients_are_not_differentiable(head):
     dx, = torch.autograd.grad(loss.sum(), x, create_graph=True)
     with pytest.raises(RuntimeError):
         dx.square().sum().backward()
+
+
+@pytest.mark.parametrize("dt", list(DT))
+@pytest.mark.parametrize("n,v,h,chunk", [(2100, 300, 130, 0), (2100, 70, 33, 1600), (70, 70001, 40, 0), (70, 20011, 200, 0)])
+def test_dw_in_parts(head, dt, n, v, h, chunk):
+    """few tiles and many tokens, or tiles past the last whole round: dw is summed in parts"""
+    x, w, t = inputs(n, v, h, dt, 20, skip=0.1)
+    check(head.linear_xent_step(x, w, t, chunk=chunk), x, w, t, None, dt, v)
