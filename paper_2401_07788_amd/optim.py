@@ -12,23 +12,40 @@ import torch
 
 from . import tc
 
+_WORDS, _N, _POS = C.sizeof(tc.Tensor) // 8, tc.Tensor.n.offset // 8, tc.Tensor.pos.offset // 8     # a row of the library's table
+
 BLOCK = 256     # positions of 8-bit moments that share an exponent
 
 _PY_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtc_py.so")
 _py = None
 
 
-def _addresses():
-    """tc_py_addresses of libtc_py.so (csrc/py_tensors.cpp)"""
+def _native():
+    """(tc_py_addresses, tc_py_table) of libtc_py.so (csrc/py_tensors.cpp)"""
     global _py
     if _py is None:
         if not os.path.exists(_PY_PATH):
             raise RuntimeError(f"{_PY_PATH} is missing: build it with paper_2401_07788_amd.build.build()")
-        f = C.PyDLL(_PY_PATH).tc_py_addresses
-        f.restype = C.c_int
+        lib = C.PyDLL(_PY_PATH)
+        f, g = lib.tc_py_addresses, lib.tc_py_table
+        f.restype, g.restype = C.c_int, C.py_object
         f.argtypes = [C.py_object, C.c_int64, C.c_void_p, C.c_int, C.c_void_p, C.c_int64]
-        _py = f
+        g.argtypes = [C.py_object, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_void_p]
+        _py = f, g
     return _py
+
+
+def _table(ts, column: int, sizes, what: str):
+    """(table of a list with the tensors' addresses in a column, their
+    elements and positions, what keeps their memory); sizes: filled too, or None"""
+    if ts and ts[0].dtype not in tc._DT:
+        raise TypeError(f"unsupported dtype {ts[0].dtype}")
+    table = (tc.Tensor * len(ts))()
+    held = _native()[1](ts, C.addressof(table), _WORDS, column, _N, _POS, sizes) if ts else None
+    if held is None:
+        _check_tensors(ts, what)
+        raise ValueError(f"{what}: dense tensors with memory of their own are needed")
+    return table, held
 
 
 def _check_tensors(ts, what: str):
@@ -54,11 +71,9 @@ class TensorList:
     (a tensor whose .data is replaced later needs a new list)."""
 
     def __init__(self, tensors):
-        self.tensors = [t.detach() for t in tensors]
-        self.dtype, self.device = _check_tensors(self.tensors, "tensors")
-        self.table = (tc.Tensor * len(self.tensors))()
-        for row, t in zip(self.table, self.tensors):
-            row.g, row.n = t.data_ptr(), t.numel()
+        self.tensors = list(tensors)
+        self.table, self._held = _table(self.tensors, 1, None, "tensors")
+        self.dtype, self.device = self.tensors[0].dtype, self.tensors[0].device
         self.ws_bytes = int(tc.lib().tc_grad_norm_workspace_bytes(len(self.tensors)))
 
 
@@ -101,30 +116,29 @@ class AdamW:
     def __init__(self, params, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
                  state_bits: int = 32, master: bool = False, state: dict = None, t: int = 0, seed: int = 0):
         self.params = list(params)
-        self.dtype, self.device = _check_tensors(self.params, "params")
+        self.sizes = (C.c_int64 * len(self.params))()
+        self.table, _ = _table(self.params, 0, self.sizes, "params")
+        self.dtype, self.device = self.params[0].dtype, self.params[0].device
         if state_bits not in (8, 32):
             raise ValueError(f"state_bits {state_bits}, not 8 or 32")
         self.lr, self.betas, self.eps, self.weight_decay = lr, betas, eps, weight_decay
         self.bits, self.t, self.seed = state_bits, t, seed
         self.places, size = [], 0
-        for p in self.params:
+        for n in self.sizes:
             self.places.append(size)
-            size += -(-p.numel() // BLOCK) * BLOCK
+            size += -(-n // BLOCK) * BLOCK
         self.size = size
         self.state = state if state is not None else self._zeros()
         self._check_state()
         self.w32 = [p.detach().float() for p in self.params] if master and self.dtype != torch.float32 else None
-        self.sizes = (C.c_int64 * len(self.params))(*[p.numel() for p in self.params])
-        self.table = (tc.Tensor * len(self.params))()
-        for k, row in enumerate(self.table):
-            row.n, row.pos = self.sizes[k], self.places[k]
-            row.w32 = self.w32[k].data_ptr() if self.w32 else None
+        for row, w in zip(self.table, self.w32 or ()):
+            row.w32 = w.data_ptr()
 
     def _fill(self, tensors, column: int):
         """the tensors' addresses into the table (0: p, 1: g); their dtype as
         the library numbers it, or -1 where they are not what they must be"""
-        return _addresses()(tensors, len(self.table), self.sizes, self.device.index, C.addressof(self.table) + 8 * column,
-                            C.sizeof(tc.Tensor) // 8)
+        return _native()[0](tensors, len(self.table), self.sizes, self.device.index, C.addressof(self.table) + 8 * column,
+                            _WORDS)
 
     def _refuse(self, grads):
         """what is wrong with the tensors of a step"""
