@@ -222,16 +222,44 @@ __global__ __launch_bounds__(BNT) void k_head_begin(const HeadArgs a) {
   const uint32_t b = blockIdx.x - 1u, lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
   const bool of_w = b >= a.top_x;
   const uint64_t rows = of_w ? a.v : a.n, first = of_w ? b - a.top_x : b, step = (of_w ? a.top_w : a.top_x) * (uint64_t)(BNT / WAVE);
-  // (a wavefront takes several short rows at a time)
+  // A lane takes 4 consecutive elements, a wavefront several short rows at a
+  // time, and 4 rows' loads go out together (32000 x 768: 76 -> 30 us).
+  constexpr uint32_t ROWS = 4;
+  struct __attribute__((packed, aligned(4))) Run { float v[4]; };
   uint32_t wide = 64;
-  while (wide > 1 && wide / 2 >= a.h) wide /= 2;
-  const uint32_t at_once = 64 / wide;
+  while (wide > 1 && wide / 2 * 4 >= a.h) wide /= 2;
+  const uint32_t at_once = 64 / wide, k0 = (lane & (wide - 1)) * 4;
   uint32_t top = 0;
-  for (uint64_t r = (first * (BNT / WAVE) + wave) * at_once + lane / wide; r < rows; r += step * at_once) {
-    if (!of_w && !has_target(a, a.target[r])) continue;
-    const float* p = of_w ? (const float*)a.w + r * a.ldw : (const float*)a.x + r * a.ldx;
-#pragma unroll 8
-    for (uint32_t k = lane & (wide - 1); k < a.h; k += wide) top = max(top, magnitude(p[k]));
+  for (uint64_t r = (first * (BNT / WAVE) + wave) * at_once + lane / wide; r < rows; r += step * at_once * ROWS) {
+    const float* p[ROWS];
+#pragma unroll
+    for (uint32_t q = 0; q < ROWS; ++q) {
+      // (a row that is not looked at: the one before it again, or none)
+      const uint64_t row = r + q * step * at_once;
+      const bool counts = row < rows && (of_w || has_target(a, a.target[row]));
+      const float* own = of_w ? (const float*)a.w + row * a.ldw : (const float*)a.x + row * a.ldx;
+      p[q] = counts ? own : q > 0 ? p[q - 1] : nullptr;
+    }
+#pragma unroll
+    for (uint32_t q = ROWS - 1; q > 0; --q)
+      if (!p[q - 1]) p[q - 1] = p[q];
+    if (!p[0]) continue;
+#pragma unroll 2
+    for (uint32_t k = k0; k < a.h; k += wide * 4) {
+      if (k + 4 <= a.h) {
+        Run v[ROWS];
+#pragma unroll
+        for (uint32_t q = 0; q < ROWS; ++q) v[q] = *reinterpret_cast<const Run*>(p[q] + k);
+#pragma unroll
+        for (uint32_t q = 0; q < ROWS; ++q)
+#pragma unroll
+          for (uint32_t z = 0; z < 4; ++z) top = max(top, magnitude(v[q].v[z]));
+      } else {
+        for (uint32_t z = k; z < a.h; ++z)
+#pragma unroll
+          for (uint32_t q = 0; q < ROWS; ++q) top = max(top, magnitude(p[q][z]));
+      }
+    }
   }
   top = block_max<BNT>(top);
   if (threadIdx.x == 0) a.tops[b] = top;
