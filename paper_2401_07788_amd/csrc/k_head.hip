@@ -71,6 +71,13 @@ template <typename T> struct Numerator<T, true> {
 
 template <typename T, int J> constexpr bool WIDE = J == 64 || std::is_same_v<T, float>;
 
+// A second plane of d in 16-bit types: what its rounding took.  Over many tokens
+// that averages out of dw (its error against 64 bits is sqrt 2 times that of
+// rounding exact sums); where up to LOW_TOKENS are left, dw, whose rows then
+// often hold one token's entry, sums both planes.  Chunks of more than
+// LOW_CHUNK tokens have no room for it.
+constexpr uint32_t LOW_TOKENS = 512, LOW_CHUNK = 2048;
+
 template <typename V8, int J> struct Cfg;
 // 256 x 256, one workgroup of 8 wavefronts per compute unit.  For fewer tokens
 // 128 x 128 and 128 x 64, two of 4 and 2 wavefronts: those products are bound
@@ -103,7 +110,7 @@ __device__ __forceinline__ uint32_t magnitude(float v) {
 // exponent that scales a binary32 operand: the largest magnitude becomes 2^14 .. 2^15
 __device__ __forceinline__ int plane_exp(uint32_t top) { return top == 0 ? 0 : 14 - ((int)(top >> 23) - 127); }
 
-constexpr float LOG2E = 1.44269504f;
+constexpr float LOG2E = 1.44269504f, LN2 = 0.693147181f;
 
 template <typename T>
 __device__ __forceinline__ uint16_t narrow(float v) {
@@ -439,7 +446,6 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
           for (int r = 0; r < 16; ++r)
             if (goal == x * 32 + h * 16 + r) a.zt[j] = acc[x][y][r];
       }
-      // one rounding of top * log2 e is common to the piece: it moves its part of lse by 2^-24 of top
       float sum = 0.0f;
       // (a piece of logits that are all -inf adds nothing)
       const float shift = top > -__builtin_inff() ? -top * LOG2E : 0.0f;
@@ -471,6 +477,9 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
         }
       }
       sum += __shfl_xor(sum, 32);
+      // the rounding of top * log2 e is common to the piece's terms: taken out of their sum again
+      // (else it would move a small loss by 2^-24 of the logit)
+      if (top > -__builtin_inff()) sum -= sum * (__builtin_fmaf(top, LOG2E, shift) * LN2);
       if (h == 0 && j < left) a.stats[(uint64_t)piece * a.chunk + j] = make_float2(top, sum);
     }
   };
@@ -484,11 +493,13 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
 }
 
 // ------------------------------------------------- pieces joined, the losses
-// and what d needs to know of a token: lse, weight (share: as a share of the
-// largest, for binary16's range) and target
+// and what d needs to know of a token: lse, target, d at the target before the
+// weight, and the weight as a share of the largest (for binary16's range; and
+// with equal weights the entries of unlikely targets are nearly -1 and not all
+// off by the rounding of one weight)
 constexpr int SNT = 1024, SR = 16;     // threads, tokens of a workgroup
 
-__global__ __launch_bounds__(SNT) void k_head_loss(const HeadArgs a, uint32_t c0, uint32_t pieces, bool share) {
+__global__ __launch_bounds__(SNT) void k_head_loss(const HeadArgs a, uint32_t c0, uint32_t pieces) {
   __shared__ float2 part[SNT / SR][SR];
   const uint32_t left = chunk_tokens(a, c0);
   const uint32_t r = threadIdx.x % SR, q = threadIdx.x / SR, j = blockIdx.x * SR + r;
@@ -528,14 +539,15 @@ __global__ __launch_bounds__(SNT) void k_head_loss(const HeadArgs a, uint32_t c0
   }
   const uint32_t jj = blockIdx.x * SR + rr;
   if (rr < SR && qq == 0 && jj < left) {
-    const float lse = m + logf(s);
+    // (the difference first: a small loss is not the difference of two large numbers)
+    const float log_s = logf(s), lse = m + log_s, loss = (m - a.zt[jj]) + log_s;
     const uint32_t i = a.rows[c0 + jj];
     a.lse[i] = lse;
-    a.loss[i] = lse - a.zt[jj];
+    a.loss[i] = loss;
     if (a.row_info) {
       const float g = a.weight ? a.weight[i] : 1.0f, most = __uint_as_float(((const Info*)a.info)->top_g);
-      const float weight = !share ? g : most > 0.0f ? g / most : g;
-      a.row_info[jj] = make_float4(lse, weight, __uint_as_float((uint32_t)a.target[i]), 0.0f);
+      const float weight = most > 0.0f ? g / most : g;
+      a.row_info[jj] = make_float4(lse, weight, __uint_as_float((uint32_t)a.target[i]), expm1f(-loss));
     }
   }
 }
@@ -544,9 +556,9 @@ __global__ __launch_bounds__(SNT) void k_head_loss(const HeadArgs a, uint32_t c0
 // A workgroup takes 128 tokens by up to 256 vocabulary entries, a lane half a
 // row of a block (32 bytes) at a time: one pass over the memory, bound by it.
 
-template <typename T, int J>
-__global__ __launch_bounds__(256) void k_head_softmax(const HeadArgs a, uint32_t c0, uint32_t piece_bits, uint32_t blocks) {
-  constexpr int PL = Type<T>::PLANES;
+template <typename T, int J, bool LOW>
+__global__ __launch_bounds__(256, 5) void k_head_softmax(const HeadArgs a, uint32_t c0, uint32_t piece_bits, uint32_t blocks) {
+  constexpr int PL = LOW ? 2 : Type<T>::PLANES;
   using N = Numerator<T, WIDE<T, J>>;
   using R = typename N::R;
   // (the tokens that the logits' kernel wrote last, and the caches may hold, first)
@@ -554,6 +566,8 @@ __global__ __launch_bounds__(256) void k_head_softmax(const HeadArgs a, uint32_t
   // (rows that fill the last stage of the sum over tokens are zeros)
   if (j >= (left + KSTAGE - 1) / KSTAGE * KSTAGE) return;
   const bool in = j < left;
+  using D = std::conditional_t<std::is_same_v<T, float>, f16_t, T>;
+  const int planes = LOW && left > LOW_TOKENS ? 1 : PL;
   const float4 row = in ? a.row_info[j] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   const uint32_t goal = __float_as_uint(row.z);
   const float w = row.y * P_SCALE<T>;
@@ -570,18 +584,28 @@ __global__ __launch_bounds__(256) void k_head_softmax(const HeadArgs a, uint32_t
         __builtin_memcpy(n, a.pt + (at + (WIDE<T, J> ? piece : place)) * sizeof(n), sizeof(n));
 #pragma unroll
         for (uint32_t y = 0; y < 8; ++y) {
-          const bool hot = kb * 32u + piece * 8u + y == goal;
-          const float p = (N::up(n[y], f) - (hot ? 1.0f : 0.0f)) * w;
+          const float p = N::up(n[y], f) * w;
           const uint16_t hi = narrow<T>(p);
           v[0][z * 8 + y] = hi;
-          // (the largest entry of most tokens: dx adds what its rounding took)
-          if (PL == 1 && hot) a.rest[j] = p - Elem<T>::up(hi);
-          if constexpr (PL == 2) v[1][z * 8 + y] = narrow<T>(p - Elem<f16_t>::up(hi));
+          if constexpr (PL == 2) v[1][z * 8 + y] = narrow<T>(p - Elem<D>::up(hi));
         }
       }
     }
 #pragma unroll
-    for (int l = 0; l < PL; ++l) __builtin_memcpy(a.pr + l * a.pr_plane + (at + 2u * half) * 16u, v[l], 32);
+    for (int l = 0; l < PL; ++l)
+      if (l < planes) __builtin_memcpy(a.pr + l * a.pr_plane + (at + 2u * half) * 16u, v[l], 32);
+    // the target's entry, from the loss (its numerator less 1 would be a small
+    // difference) and after the others (no entry is compared with the target)
+    if (in && goal >> 5 == kb && (((goal >> 3 & 3u) ^ turn(j)) >> 1) == half) {
+      const float p = row.w * w;
+      const uint16_t hi = narrow<T>(p);
+      const float low = p - Elem<D>::up(hi);
+      char* o = a.pr + (at + ((goal >> 3 & 3u) ^ turn(j))) * 16u + (goal & 7u) * 2u;
+      *reinterpret_cast<uint16_t*>(o) = hi;
+      // (the largest entry of most tokens: dx adds what its rounding took)
+      if (Type<T>::PLANES == 1) a.rest[j] = low;
+      if (PL == 2 && planes == 2) *reinterpret_cast<uint16_t*>(o + a.pr_plane) = narrow<T>(low);
+    }
   }
 }
 
@@ -660,7 +684,7 @@ __global__ __launch_bounds__(256) void k_head_dx_sum(const HeadArgs a, uint32_t 
     return;
   }
   float f = 1.0f / P_SCALE<T>;
-  if (!std::is_same_v<T, bf16_t>) f *= __uint_as_float(info.top_g);
+  f *= __uint_as_float(info.top_g);
   if (Type<T>::PLANES == 2) f = __builtin_ldexpf(f, -plane_exp(info.top_w));
   const uint32_t left = chunk_tokens(a, c0), splits = DxPlan(a, left, ti, tj, Type<T>::PLANES == 2 ? 3 : 1).splits;
   const float rest = Type<T>::PLANES == 1 ? a.rest[j] : 0.0f;
@@ -689,7 +713,7 @@ struct DwPlan {
     nj = ((uint32_t)a.v + G::TJ - 1) / G::TJ;
     whole = a.dw_parts ? ni * nj / a.dw_grid * a.dw_grid : ni * nj;
     rest = ni * nj - whole;
-    all = (Type<T>::PLANES == 2 ? 3 : 1) * ((left + KSTAGE - 1) / KSTAGE);
+    all = (Type<T>::PLANES == 2 ? 3 : a.d_low && left <= LOW_TOKENS ? 2 : 1) * ((left + KSTAGE - 1) / KSTAGE);
     parts = min(a.dw_parts, all);       // (each has a stage at least)
   }
   __device__ __forceinline__ Tile tile(uint32_t t) const {
@@ -836,12 +860,12 @@ template <typename T>
 __device__ __forceinline__ float dw_factor(const HeadArgs& a) {
   const Info info = *(const Info*)a.info;
   float f = 1.0f / P_SCALE<T>;
-  if (!std::is_same_v<T, bf16_t>) f *= __uint_as_float(info.top_g);
+  f *= __uint_as_float(info.top_g);
   if (Type<T>::PLANES == 2) f = __builtin_ldexpf(f, -plane_exp(info.top_x));
   return f;
 }
 
-template <typename T, int W>
+template <typename T, int W, bool LOW>
 __global__ __launch_bounds__((Cfg<typename Type<T>::V8, W>::NT), 2) void k_head_dw(const HeadArgs a, uint32_t c0) {
   using G = Cfg<typename Type<T>::V8, W>;
   extern __shared__ __attribute__((aligned(128))) char lds[];
@@ -902,7 +926,7 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, W>::NT), 2) void k_head_
     return true;
   };
   const BlocksT A{a.xr, a.c_blocks, a.xr_plane}, B{a.pr, a.c_blocks, a.pr_plane};
-  G::template stream<Type<T>::PLANES == 2 ? 3 : 1>(A, B, (left + KSTAGE - 1) / KSTAGE, lds, work, done);
+  G::template stream<Type<T>::PLANES == 2 ? 3 : LOW ? 2 : 1>(A, B, (left + KSTAGE - 1) / KSTAGE, lds, work, done);
 }
 
 // one fragment row of a tile of the last round per workgroup
@@ -975,7 +999,9 @@ bool alone(const HeadArgs& a) { return Type<T>::PLANES == 1 && a.n <= ALONE_TOKE
 template <typename T, int W>
 hipError_t launch_dw(const HeadArgs& a, uint32_t c0, hipStream_t st) {
   using G = Cfg<typename Type<T>::V8, W>;
-  HEAD_TRY((launch_lds<k_head_dw<T, W>>(a.dw_grid, G::NT, G::LDS + G::NW * RUN_LDS, st, a, c0)));
+  constexpr uint32_t LDS = G::LDS + G::NW * RUN_LDS;
+  HEAD_TRY((a.d_low ? launch_lds<k_head_dw<T, W, Type<T>::PLANES == 1>>(a.dw_grid, G::NT, LDS, st, a, c0)
+                    : launch_lds<k_head_dw<T, W, false>>(a.dw_grid, G::NT, LDS, st, a, c0)));
   if (a.dw_parts) {
     const uint32_t tiles = ((a.h + G::TI - 1) / G::TI) * (((uint32_t)a.v + G::TJ - 1) / G::TJ);
     hipLaunchKernelGGL((k_head_dw_tail<T, W>), dim3(tiles % a.dw_grid * (G::WI * G::WJ)), dim3(G::NT), 0, st, a, c0);
@@ -1008,13 +1034,12 @@ hipError_t chunk_of(HeadArgs& a, uint32_t c0, uint32_t rows, hipStream_t st) {
   } else {
     HEAD_TRY((launch_lds<k_head_logits<T, J, GRAD, false>>(grid_of<G>(ni * nj), G::NT, G::LDS, st, a, c0)));
   }
-  hipLaunchKernelGGL(k_head_loss, dim3((rows + SR - 1) / SR), dim3(SNT), 0, st, a, c0, pieces,
-                     !std::is_same_v<T, bf16_t>);
+  hipLaunchKernelGGL(k_head_loss, dim3((rows + SR - 1) / SR), dim3(SNT), 0, st, a, c0, pieces);
   HEAD_TRY(hipGetLastError());
   if constexpr (GRAD) {
     const uint32_t high = (rows + 127) / 128, blocks = std::max(1u, std::min(4u, a.k_dx * high / 2048u));
-    hipLaunchKernelGGL((k_head_softmax<T, J>), dim3((a.k_dx + blocks - 1) / blocks, high), dim3(256), 0, st, a, c0,
-                       PIECE == 128 ? 7u : 6u, blocks);
+    const auto softmax = a.d_low ? k_head_softmax<T, J, Type<T>::PLANES == 1> : k_head_softmax<T, J, false>;
+    hipLaunchKernelGGL(softmax, dim3((a.k_dx + blocks - 1) / blocks, high), dim3(256), 0, st, a, c0, PIECE == 128 ? 7u : 6u, blocks);
     HEAD_TRY(hipGetLastError());
     HEAD_TRY((launch_lds<k_head_dx<T, J>>(a.dx_grid, G::NT, G::LDS, st, a, c0)));
     if (a.n > 0) {
@@ -1094,7 +1119,8 @@ uint64_t head_plan(HeadArgs& a, int dt, bool grad, char* base) {
   a.xr = take(planes * a.xr_plane);
   if (grad) {
     a.pr_plane = a.c_blocks * kv * 1024;
-    a.pr = take(planes * a.pr_plane);
+    a.d_low = planes == 1 && a.chunk <= LOW_CHUNK;
+    a.pr = take((a.d_low ? 2 : planes) * a.pr_plane);
     a.pt = planes == 2 || a.chunk <= 64 ? take(a.pr_plane * 2) : a.pr;
     a.row_info = (float4*)take(a.chunk * 16);
     a.rest = (float*)take(a.chunk * 4);
@@ -1121,7 +1147,7 @@ uint64_t head_plan(HeadArgs& a, int dt, bool grad, char* base) {
     const uint64_t cus = (uint64_t)(device_cus() + 7) / 8 * 8;
     a.dw_small = (a.h + 255) / 256 * ((a.v + 255) / 256) * 3 <= cus;
     const uint64_t wi = a.dw_small ? 128 : 256, wj = a.dw_small ? 64 : 256, slots = a.dw_small ? 2 * cus : cus;
-    const uint64_t wt = (a.h + wi - 1) / wi * ((a.v + wj - 1) / wj), rows = (planes == 2 ? 3 : 1) * ((a.chunk + KSTAGE - 1) / KSTAGE);
+    const uint64_t wt = (a.h + wi - 1) / wi * ((a.v + wj - 1) / wj), rows = (planes == 2 ? 3 : a.d_low && a.chunk <= LOW_TOKENS ? 2 : 1) * ((a.chunk + KSTAGE - 1) / KSTAGE);
     a.dw_grid = (uint32_t)std::min<uint64_t>(slots, (wt + 7) / 8 * 8);
     a.dw_parts = 0;
     if (wt < slots) {

@@ -205,7 +205,7 @@ struct Gemm {
   };
 
   // A piece of work: stages [s0, s0 + count) of the tile at (i0, j0), count > 0.
-  // The walk along k goes over the pairs of planes (one, or three: high high,
+  // The walk along k goes over the pairs of planes (up to PAIRS of high high,
   // high low, low high), `per` stages each.
   struct Work {
     uint32_t i0, j0, s0, count;

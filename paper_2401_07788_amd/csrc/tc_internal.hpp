@@ -184,7 +184,7 @@ struct HeadArgs {
   uint32_t* rows;        // [n] tokens that have a target, then the others
   uint32_t* tops;
   float* zt;             // [chunk] logit of the target
-  float4* row_info;      // [chunk] lse, weight, target (gradients only)
+  float4* row_info;      // [chunk] lse, weight, target, d at the target (gradients only)
   float* rest;           // [chunk] what rounding took from d's entry at the target
   float2* stats;         // [pieces][chunk] maximum and sum of a piece of the vocabulary
   // in blocks (tc_gemm.hpp), rows by elements of a row
@@ -194,6 +194,7 @@ struct HeadArgs {
   float* dx_part;        // [splits][chunk][hq]
   float* dw_sum;         // [v][hq], or nullptr with one chunk
   uint32_t dw_grid, dw_parts;   // workgroups of dw's product; parts of its last round's tiles
+  bool d_low;                   // d has a second plane of 16 bits (16-bit types)
   bool dw_small;                // 128 x 64 tiles, not 256 x 256
   float* dw_part;        // [tiles of the last round][dw_parts][a tile]
 };

@@ -380,3 +380,35 @@ def test_dw_in_parts(head, dt, n, v, h, chunk):
     """few tiles and many tokens, or tiles past the last whole round: dw is summed in parts"""
     x, w, t = inputs(n, v, h, dt, 20, skip=0.1)
     check(head.linear_xent_step(x, w, t, chunk=chunk), x, w, t, None, dt, v)
+
+
+@pytest.mark.parametrize("dt", list(DT))
+def test_small_losses(head, dt):
+    """tokens that the model is sure of: a loss of 1e-3 or less next to logits of 30 is not their difference"""
+    n, v, h = 60, 300, 64
+    x, w, t = inputs(n, v, h, dt, 21)
+    wt = w[t].float()
+    x = (wt * (30 / wt.square().sum(1, keepdim=True))).to(DT[dt])
+    loss, _ = head.linear_xent(x, w, t)
+    want, _ = reference(x, w, t, None, v)
+    want = want["loss"]
+    assert float(want.median()) < 1e-3
+    # the logits' errors (of sums of h terms, up to 30) move the other terms of the sum, which are the loss; the
+    # sum near 1, its correction and the logarithm: four roundings
+    lim = want * (2 * (4 * math.sqrt(h) + 8) * 2.0 ** -24 * 60 + 2.0 ** -16) + 4 * 2.0 ** -24
+    assert bool(((loss.double().cpu() - want).abs() <= lim).all())
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("n,skip", [(1, 0.0), (7, 0.0), (1100, 0.7)])
+def test_dw_of_few_tokens(head, dt, n, skip):
+    """the roundings of few entries of d do not average out: dw is as exact as its own rounding"""
+    v, h = 400, 96
+    x, w, t = inputs(n, v, h, dt, 22, skip=skip)
+    weight = torch.full((n,), 1 / 3.0, device="cuda")
+    r = head.linear_xent_step(x, w, t, weight)
+    want, size = reference(x, w, t, weight, v)
+    # two planes of d: its entries to 2^-14 (numerators in 16 bits over more than 128 tokens: 2^-10), logits to 2^-14
+    rel = 2.0 ** -12 if n <= 128 else 2.0 ** -9
+    lim = U[dt] * want["dw"].abs() + rel * size["dw"] + (2.0 ** -24 if dt == "f16" else 1e-38) + 2.0 ** -36 * size["x"]
+    assert bool(((r.dw.double().cpu() - want["dw"]).abs() <= lim).all())
