@@ -360,8 +360,10 @@ tc_status tc_xent_loss(const tc_xent* c, const void* x, const void* w, const int
  * weight: [n] binary32, or NULL (1).  Into the two products d goes as a share
  * of the largest |weight| with the significand of dt (binary32: 22 bits; into
  * dw twice that of the 16-bit types where up to 512 tokens of a chunk of up to
- * 2048 count); bfloat16 keeps its range, binary16 and binary32 reach down to
- * 2^-28 of the largest in full and to 2^-38 at the least. */
+ * 2048 count); bfloat16 keeps its range (down to 2^-126), binary16 and
+ * binary32 reach down to 2^-28 of the largest in full and to 2^-38 at the
+ * least.  Logits may be as large as binary32 holds: loss and d follow from
+ * their differences. */
 tc_status tc_xent_step(const tc_xent* c, const void* x, const void* w, const int64_t* target, const float* weight,
                        float* loss, float* lse, void* dx, void* dw, void* ws, size_t ws_bytes, void* stream);
 

@@ -110,7 +110,7 @@ __device__ __forceinline__ uint32_t magnitude(float v) {
 // exponent that scales a binary32 operand: the largest magnitude becomes 2^14 .. 2^15
 __device__ __forceinline__ int plane_exp(uint32_t top) { return top == 0 ? 0 : 14 - ((int)(top >> 23) - 127); }
 
-constexpr float LOG2E = 1.44269504f, LN2 = 0.693147181f;
+constexpr float LOG2E = 1.44269504f;
 
 template <typename T>
 __device__ __forceinline__ uint16_t narrow(float v) {
@@ -447,13 +447,17 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
             if (goal == x * 32 + h * 16 + r) a.zt[j] = acc[x][y][r];
       }
       float sum = 0.0f;
+      // The maximum comes off before the scaling: its entry is 1 exactly and no
+      // other is more, whatever the logits' size (off the scaled one, rounding
+      // would move all entries by 2^-24 of the logit in the exponent, and from
+      // logits of 1e7 on the largest out of a numerator's range).
       // (a piece of logits that are all -inf adds nothing)
-      const float shift = top > -__builtin_inff() ? -top * LOG2E : 0.0f;
+      const float base = top > -__builtin_inff() ? top : 0.0f;
 #pragma unroll
       for (int x = 0; x < G::WI; ++x) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[x][y][r], LOG2E, shift));
+          const float p = __builtin_amdgcn_exp2f((acc[x][y][r] - base) * LOG2E);
           acc[x][y][r] = p;
           sum += p;
         }
@@ -477,9 +481,6 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
         }
       }
       sum += __shfl_xor(sum, 32);
-      // the rounding of top * log2 e is common to the piece's terms: taken out of their sum again
-      // (else it would move a small loss by 2^-24 of the logit)
-      if (top > -__builtin_inff()) sum -= sum * (__builtin_fmaf(top, LOG2E, shift) * LN2);
       if (h == 0 && j < left) a.stats[(uint64_t)piece * a.chunk + j] = make_float2(top, sum);
     }
   };
@@ -493,10 +494,12 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
 }
 
 // ------------------------------------------------- pieces joined, the losses
-// and what d needs to know of a token: lse, target, d at the target before the
-// weight, and the weight as a share of the largest (for binary16's range; and
-// with equal weights the entries of unlikely targets are nearly -1 and not all
-// off by the rounding of one weight)
+// and what d needs to know of a token: the largest logit, the weight over the
+// sum of exponentials, the target, and d at the target.  (lse would do for the
+// first two, but of large logits it is known to 2^-24 of their size only.)  The
+// weight is a share of the largest (for binary16's range; and with equal
+// weights the entries of unlikely targets are nearly -1 and not all off by the
+// rounding of one weight).
 constexpr int SNT = 1024, SR = 16;     // threads, tokens of a workgroup
 
 __global__ __launch_bounds__(SNT) void k_head_loss(const HeadArgs a, uint32_t c0, uint32_t pieces) {
@@ -547,7 +550,7 @@ __global__ __launch_bounds__(SNT) void k_head_loss(const HeadArgs a, uint32_t c0
     if (a.row_info) {
       const float g = a.weight ? a.weight[i] : 1.0f, most = __uint_as_float(((const Info*)a.info)->top_g);
       const float weight = most > 0.0f ? g / most : g;
-      a.row_info[jj] = make_float4(lse, weight, __uint_as_float((uint32_t)a.target[i]), expm1f(-loss));
+      a.row_info[jj] = make_float4(m, weight / s, __uint_as_float((uint32_t)a.target[i]), expm1f(-loss) * weight);
     }
   }
 }
@@ -597,7 +600,7 @@ __global__ __launch_bounds__(256, 5) void k_head_softmax(const HeadArgs a, uint3
     // the target's entry, from the loss (its numerator less 1 would be a small
     // difference) and after the others (no entry is compared with the target)
     if (in && goal >> 5 == kb && (((goal >> 3 & 3u) ^ turn(j)) >> 1) == half) {
-      const float p = row.w * w;
+      const float p = row.w * P_SCALE<T>;
       const uint16_t hi = narrow<T>(p);
       const float low = p - Elem<D>::up(hi);
       char* o = a.pr + (at + ((goal >> 3 & 3u) ^ turn(j))) * 16u + (goal & 7u) * 2u;

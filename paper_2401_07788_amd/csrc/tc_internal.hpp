@@ -184,7 +184,7 @@ struct HeadArgs {
   uint32_t* rows;        // [n] tokens that have a target, then the others
   uint32_t* tops;
   float* zt;             // [chunk] logit of the target
-  float4* row_info;      // [chunk] lse, weight, target, d at the target (gradients only)
+  float4* row_info;      // [chunk] largest logit, weight over the sum, target, d at the target (gradients only)
   float* rest;           // [chunk] what rounding took from d's entry at the target
   float2* stats;         // [pieces][chunk] maximum and sum of a piece of the vocabulary
   // in blocks (tc_gemm.hpp), rows by elements of a row

@@ -412,3 +412,53 @@ def test_dw_of_few_tokens(head, dt, n, skip):
     rel = 2.0 ** -12 if n <= 128 else 2.0 ** -9
     lim = U[dt] * want["dw"].abs() + rel * size["dw"] + (2.0 ** -24 if dt == "f16" else 1e-38) + 2.0 ** -36 * size["x"]
     assert bool(((r.dw.double().cpu() - want["dw"]).abs() <= lim).all())
+
+
+def large_logits(n, v, dt, size, sign, on_target):
+    """logits of about sign * 2^size whose differences are whole numbers of `q`, all of them exact: token i's are
+    sign * X_i W - k_v q; one entry has k = 0 and stands alone on top, by 1 to 200 q"""
+    g = torch.Generator(device="cuda").manual_seed(size + n)
+    half = size // 2
+    q = 2.0 ** max(size - 20, -4)        # 2^-20 of the logits at the least: a sum of binary32 holds them
+    x, w = torch.zeros(n, 40, device="cuda"), torch.zeros(v, 40, device="cuda")
+    x[:, 0] = (128 + torch.arange(n, device="cuda") % 120) * 2.0 ** (half - 8) * sign
+    x[:, 1] = 1.0
+    w[:, 0] = 179 * 2.0 ** (size - half - 8)
+    k = torch.randint(1, 201, (v,), generator=g, device="cuda")
+    top = v // 3
+    k[top] = 0
+    w[:, 1] = -q * k
+    t = torch.randint(0, v, (n,), generator=g, device="cuda")
+    t[t == top] = top + 1
+    if on_target:
+        t[::2] = top
+    return x.to(DT[dt]), w.to(DT[dt]), t
+
+
+@pytest.mark.parametrize("n", [40, 100, 200])
+@pytest.mark.parametrize("on_target", [True, False])
+@pytest.mark.parametrize("dt,size", [(dt, size) for dt in DT for size in (12, 20, 25, 28)] + [("f32", 60), ("bf16", 60)])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_large_logits(head, dt, n, on_target, size, sign):
+    """the softmax depends on differences of the logits, however large they are"""
+    v = 300
+    x, w, t = large_logits(n, v, dt, size, sign, on_target)
+    weight = (torch.rand(n, device="cuda") + 0.5) / n
+    r = head.linear_xent_step(x, w, t, weight)
+    want, bound = reference(x, w, t, weight, v)
+    # the logits, their maximum and the difference to the target's are exact.  The sum of exponentials, 1 at the least:
+    # two roundings of each difference d, of which d exp(-d) <= 0.37 reaches the sum, the exponential's and 300 of the sum
+    lim = 2.0 ** -18 + 2.0 ** -22 * want["loss"].abs()
+    assert bool((r.loss >= 0).all())
+    assert bool(((r.loss.double().cpu() - want["loss"]).abs() <= lim).all())
+    assert bool(((r.lse.double().cpu() - want["lse"]).abs() <= 2.0 ** -18 + 2.0 ** -22 * want["lse"].abs()).all())
+    loss, lse = head.linear_xent(x, w, t)
+    assert torch.equal(loss, r.loss) and torch.equal(lse, r.lse)
+    # an entry of d: its roundings, two of a difference of up to 126 (2^-16), up to 300 of a product's sum (2^-16); below
+    # 2^-126 (bfloat16: the exponential) or 2^-38 (the others' operands) of the largest weight an entry may be 0
+    rel, low = UD[dt] + 2.0 ** -14, 2.0 ** -38 if dt != "bf16" else 2.0 ** -126
+    for k, more in (("dx", w.double().cpu().abs().sum(0)), ("dw", bound["x"])):
+        got = getattr(r, k).double().cpu()
+        assert float(want[k].abs().max()) < 0.9 * torch.finfo(DT[dt]).max
+        lim = rel * bound[k] + U[dt] * want[k].abs() + (2.0 ** -24 if dt == "f16" else 1e-38) + 2 * low * bound["top"] * more
+        assert bool(((got - want[k]).abs() <= lim).all()), (k, float(((got - want[k]).abs() - lim).max()))
