@@ -112,6 +112,28 @@ __device__ __forceinline__ int plane_exp(uint32_t top) { return top == 0 ? 0 : 1
 
 constexpr float LOG2E = 1.44269504f;
 
+// A gradient from the sum of its products: times the largest weight, and the
+// operands' scalings taken back.  Of binary32 the power of two goes to the
+// product, in one step: as a factor it could lie outside of binary32 where the
+// gradient does not.
+template <typename T>
+struct OutScale {
+  float f;
+  int e;
+  __device__ __forceinline__ OutScale(uint32_t top_g, uint32_t top) {
+    if constexpr (Type<T>::PLANES == 2) {
+      f = __builtin_amdgcn_frexp_mantf(__uint_as_float(top_g));
+      e = __builtin_amdgcn_frexp_expf(__uint_as_float(top_g)) - 14 - plane_exp(top);
+    } else {
+      f = __uint_as_float(top_g) * (1.0f / P_SCALE<T>);
+    }
+  }
+  __device__ __forceinline__ float operator()(float s) const {
+    if constexpr (Type<T>::PLANES == 2) return __builtin_ldexpf(s * f, e);
+    else return s * f;
+  }
+};
+
 template <typename T>
 __device__ __forceinline__ uint16_t narrow(float v) {
   if constexpr (std::is_same_v<T, bf16_t>) return Elem<bf16_t>::down(v);
@@ -686,9 +708,7 @@ __global__ __launch_bounds__(256) void k_head_dx_sum(const HeadArgs a, uint32_t 
     for (uint32_t k = threadIdx.x; k < a.h; k += 256) o[k] = R{};
     return;
   }
-  float f = 1.0f / P_SCALE<T>;
-  f *= __uint_as_float(info.top_g);
-  if (Type<T>::PLANES == 2) f = __builtin_ldexpf(f, -plane_exp(info.top_w));
+  const OutScale<T> scaled(info.top_g, info.top_w);
   const uint32_t left = chunk_tokens(a, c0), splits = DxPlan(a, left, ti, tj, Type<T>::PLANES == 2 ? 3 : 1).splits;
   const float rest = Type<T>::PLANES == 1 ? a.rest[j] : 0.0f;
   const R* w = (const R*)a.w + (uint64_t)a.target[i] * a.ldw;
@@ -697,7 +717,7 @@ __global__ __launch_bounds__(256) void k_head_dx_sum(const HeadArgs a, uint32_t 
 #pragma unroll 4
     for (uint32_t q = 0; q < splits; ++q) s += a.dx_part[((uint64_t)q * left + j) * a.hq + k];
     if (Type<T>::PLANES == 1) s += rest * Elem<T>::up(w[k]);
-    o[k] = Elem<T>::down(s * f);
+    o[k] = Elem<T>::down(scaled(s));
   }
 }
 
@@ -726,14 +746,14 @@ struct DwPlan {
 };
 
 template <typename T>
-__device__ __forceinline__ void dw_store(const HeadArgs& a, uint32_t c0, float f, uint32_t i, uint32_t j, const float (&v)[16]) {
+__device__ __forceinline__ void dw_store(const HeadArgs& a, uint32_t c0, const OutScale<T>& scaled, uint32_t i, uint32_t j, const float (&v)[16]) {
   using R = typename Elem<T>::raw;
   if (i >= a.h || j >= a.v) return;
   if (a.dw_sum) {
     float* o = a.dw_sum + (uint64_t)j * a.hq + i;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      float4 s = make_float4(v[q * 4] * f, v[q * 4 + 1] * f, v[q * 4 + 2] * f, v[q * 4 + 3] * f);
+      float4 s = make_float4(scaled(v[q * 4]), scaled(v[q * 4 + 1]), scaled(v[q * 4 + 2]), scaled(v[q * 4 + 3]));
       if (c0 > 0) {
         const float4 old = reinterpret_cast<const float4*>(o)[q];
         s = make_float4(s.x + old.x, s.y + old.y, s.z + old.z, s.w + old.w);
@@ -743,7 +763,7 @@ __device__ __forceinline__ void dw_store(const HeadArgs& a, uint32_t c0, float f
   } else {
     R w[16];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) w[r] = Elem<T>::down(v[r] * f);
+    for (int r = 0; r < 16; ++r) w[r] = Elem<T>::down(scaled(v[r]));
     R* o = (R*)a.dw + (uint64_t)j * a.h + i;
     if (i + 16 <= a.h) {
       // (the hardware stores vectors at any element's address)
@@ -774,7 +794,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr uint32_t RUN_LDS = 4096;       // of a wavefront: 16 rows of 256 bytes
 
 template <typename T, int WI, int WJ>
-__device__ __forceinline__ void dw_store_runs(const HeadArgs& a, float f, char* lds, uint32_t lane, uint32_t i0, uint32_t j0, f32x16 (&acc)[WI][WJ]) {
+__device__ __forceinline__ void dw_store_runs(const HeadArgs& a, const OutScale<T>& scaled, char* lds, uint32_t lane, uint32_t i0, uint32_t j0, f32x16 (&acc)[WI][WJ]) {
   using R = typename Elem<T>::raw;
   // XF fragments side by side make a run (128 bytes where a wavefront has no
   // more), Q pieces of PER elements to a lane's row of each
@@ -804,7 +824,7 @@ __device__ __forceinline__ void dw_store_runs(const HeadArgs& a, float f, char* 
       for (uint32_t x = 0; x < XF; ++x) {
         R w[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = Elem<T>::down(acc[g * XF + x][y][e] * f);
+        for (int e = 0; e < 16; ++e) w[e] = Elem<T>::down(scaled(acc[g * XF + x][y][e]));
         __builtin_memcpy(v[x], w, sizeof(w));
       }
 #pragma unroll
@@ -860,12 +880,9 @@ __device__ __forceinline__ void dw_store_runs(const HeadArgs& a, float f, char* 
 }
 
 template <typename T>
-__device__ __forceinline__ float dw_factor(const HeadArgs& a) {
+__device__ __forceinline__ OutScale<T> dw_scale(const HeadArgs& a) {
   const Info info = *(const Info*)a.info;
-  float f = 1.0f / P_SCALE<T>;
-  f *= __uint_as_float(info.top_g);
-  if (Type<T>::PLANES == 2) f = __builtin_ldexpf(f, -plane_exp(info.top_x));
-  return f;
+  return OutScale<T>(info.top_g, info.top_x);
 }
 
 template <typename T, int W, bool LOW>
@@ -875,7 +892,7 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, W>::NT), 2) void k_head_
   const uint32_t left = chunk_tokens(a, c0);
   if (c0 > 0 && left == 0) return;
   const DwPlan<T, W> plan(a, left);
-  const float f = dw_factor<T>(a);
+  const OutScale<T> scaled = dw_scale<T>(a);
   const uint32_t mine = die_tile(blockIdx.x, gridDim.x);
   auto done = [&](uint32_t n, const typename G::Work& at, f32x16 (&acc)[G::WI][G::WJ]) {
     const uint32_t thread = own_thread();
@@ -883,7 +900,7 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, W>::NT), 2) void k_head_
     const uint32_t iw = at.i0 + (wave % G::NWI) * (G::WI * 32) + h * 16, jw = at.j0 + (wave / G::NWI) * (G::WJ * 32) + (lane & 31u);
     const bool part = a.dw_parts && n * gridDim.x >= plan.whole;
     if (!part && !a.dw_sum) {
-      dw_store_runs<T>(a, f, lds + G::LDS + wave * RUN_LDS, lane, iw - h * 16, jw - (lane & 31u), acc);
+      dw_store_runs<T>(a, scaled, lds + G::LDS + wave * RUN_LDS, lane, iw - h * 16, jw - (lane & 31u), acc);
       return;
     }
 #pragma unroll
@@ -900,7 +917,7 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, W>::NT), 2) void k_head_
 #pragma unroll
           for (int q = 0; q < 4; ++q) o[q * G::NT] = make_float4(v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]);
         } else {
-          dw_store<T>(a, c0, f, iw + x * 32, jw + y * 32, v);
+          dw_store<T>(a, c0, scaled, iw + x * 32, jw + y * 32, v);
         }
       }
   };
@@ -956,7 +973,7 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, W>::NT)) void k_head_dw_
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h = lane >> 5;
   const uint32_t i = at.i * G::TI + (wave % G::NWI) * (G::WI * 32) + h * 16 + x * 32;
   const uint32_t j = at.j * G::TJ + (wave / G::NWI) * (G::WJ * 32) + (lane & 31u) + y * 32;
-  dw_store<T>(a, c0, dw_factor<T>(a), i, j, v);
+  dw_store<T>(a, c0, dw_scale<T>(a), i, j, v);
 }
 
 template <typename T>

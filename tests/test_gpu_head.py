@@ -462,3 +462,13 @@ def test_large_logits(head, dt, n, on_target, size, sign):
         assert float(want[k].abs().max()) < 0.9 * torch.finfo(DT[dt]).max
         lim = rel * bound[k] + U[dt] * want[k].abs() + (2.0 ** -24 if dt == "f16" else 1e-38) + 2 * low * bound["top"] * more
         assert bool(((got - want[k]).abs() <= lim).all()), (k, float(((got - want[k]).abs() - lim).max()))
+
+
+@pytest.mark.parametrize("sx,sw", [(1e-32, 1e32), (1e32, 1e-32), (2.0 ** -110, 2.0 ** 100), (2.0 ** 100, 2.0 ** -110)])
+@pytest.mark.parametrize("n", [40, 200])
+def test_binary32_gradients_far_from_one(head, sx, sw, n):
+    """gradients that are ordinary numbers although the factors they are made of are not"""
+    x, w, t = inputs(n, 100, 64, "f32", 23)
+    x, w = x * sx, w * sw
+    weight = torch.full((n,), 1 / 3000.0, device="cuda")
+    check(head.linear_xent_step(x, w, t, weight), x, w, t, weight, "f32", 100)
