@@ -436,7 +436,7 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
     const uint32_t iw = at.i0 + (wave % G::NWI) * (G::WI * 32), jw = at.j0 + (wave / G::NWI) * (G::WJ * 32) + (lane & 31u);
     if (iw >= a.v) return;
     const uint32_t piece = iw / (G::WI * 32);
-    const float scale = Type<T>::PLANES == 2 ? __builtin_ldexpf(1.0f, -plane_exp(info.top_w) - plane_exp(info.top_x)) : 1.0f;
+    const int back = Type<T>::PLANES == 2 ? -plane_exp(info.top_w) - plane_exp(info.top_x) : 0;
     // entries past the vocabulary's end, in its last tile
     if (iw + G::WI * 32 > a.v) {
 #pragma unroll
@@ -455,7 +455,7 @@ __global__ __launch_bounds__((Cfg<typename Type<T>::V8, J>::NT), 2) void k_head_
       for (int x = 0; x < G::WI; ++x)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          if (Type<T>::PLANES == 2) acc[x][y][r] *= scale;
+          if (Type<T>::PLANES == 2) acc[x][y][r] = __builtin_ldexpf(acc[x][y][r], back);
           top = fmaxf(top, acc[x][y][r]);
         }
       top = fmaxf(top, __shfl_xor(top, 32));

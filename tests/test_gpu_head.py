@@ -472,3 +472,20 @@ def test_binary32_gradients_far_from_one(head, sx, sw, n):
     x, w = x * sx, w * sw
     weight = torch.full((n,), 1 / 3000.0, device="cuda")
     check(head.linear_xent_step(x, w, t, weight), x, w, t, weight, "f32", 100)
+
+
+def test_binary32_token_of_zeros_among_large_ones(head):
+    """its logits are 0, and stay so under the scaling that the others need"""
+    v = 100
+    x, w, t = inputs(40, v, 64, "f32", 24)
+    x, w = x * 2.0 ** 90, w * 2.0 ** 90
+    x[7] = 0.0
+    for r in (head.linear_xent_step(x, w, t), None):
+        loss = r.loss if r else head.linear_xent(x, w, t)[0]
+        assert abs(float(loss[7]) - math.log(v)) < 2.0 ** -19 * math.log(v)
+        if r:
+            d = torch.full((v,), 1.0 / v, dtype=torch.float64, device="cuda")
+            d[t[7]] -= 1
+            # d and w as pairs of binary16 (22 bits each), 100 products summed
+            lim = (2.0 ** -20 + 2.0 ** -17) * (d.abs() @ w.double().abs())
+            assert bool(((r.dx[7].double() - d @ w.double()).abs() <= lim).all())
