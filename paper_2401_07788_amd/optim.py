@@ -14,6 +14,8 @@ from . import tc
 
 _WORDS, _N, _POS = C.sizeof(tc.Tensor) // 8, tc.Tensor.n.offset // 8, tc.Tensor.pos.offset // 8     # a row of the library's table
 
+_STATE_TYPES = {torch.float32: 0, torch.uint8: 3, torch.int8: 4}     # as csrc/py_tensors.cpp numbers them
+
 BLOCK = 256     # positions of 8-bit moments that share an exponent
 
 _PY_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtc_py.so")
@@ -21,17 +23,19 @@ _py = None
 
 
 def _native():
-    """(tc_py_addresses, tc_py_table) of libtc_py.so (csrc/py_tensors.cpp)"""
+    """(tc_py_step, tc_py_table, tc_py_state) of libtc_py.so (csrc/py_tensors.cpp)"""
     global _py
     if _py is None:
         if not os.path.exists(_PY_PATH):
             raise RuntimeError(f"{_PY_PATH} is missing: build it with paper_2401_07788_amd.build.build()")
         lib = C.PyDLL(_PY_PATH)
-        f, g = lib.tc_py_addresses, lib.tc_py_table
-        f.restype, g.restype = C.c_int, C.py_object
-        f.argtypes = [C.py_object, C.c_int64, C.c_void_p, C.c_int, C.c_void_p, C.c_int64]
+        f, g, h = lib.tc_py_step, lib.tc_py_table, lib.tc_py_state
+        f.restype, g.restype, h.restype = C.c_int, C.py_object, C.c_int
+        f.argtypes = [C.py_object, C.py_object, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.py_object, C.c_int64,
+                      C.c_void_p, C.c_void_p, C.c_void_p, C.c_int]
         g.argtypes = [C.py_object, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_void_p]
-        _py = f, g
+        h.argtypes = [C.py_object, C.c_int64, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p]
+        _py = f, g, h
     return _py
 
 
@@ -122,23 +126,26 @@ class AdamW:
         if state_bits not in (8, 32):
             raise ValueError(f"state_bits {state_bits}, not 8 or 32")
         self.lr, self.betas, self.eps, self.weight_decay = lr, betas, eps, weight_decay
-        self.bits, self.t, self.seed = state_bits, t, seed
+        self._bits, self.t, self.seed = state_bits, t, seed
         self.places, size = [], 0
         for n in self.sizes:
             self.places.append(size)
             size += -(-n // BLOCK) * BLOCK
         self.size = size
+        spec = self._spec()
+        self._names, self._at = tuple(spec), (C.c_uint64 * len(spec))()
+        self._lengths = (C.c_int64 * len(spec))(*(n for n, _ in spec.values()))
+        self._types = (C.c_int8 * len(spec))(*(_STATE_TYPES[dt] for _, dt in spec.values()))
         self.state = state if state is not None else self._zeros()
         self._check_state()
         self.w32 = [p.detach().float() for p in self.params] if master and self.dtype != torch.float32 else None
         for row, w in zip(self.table, self.w32 or ()):
             row.w32 = w.data_ptr()
 
-    def _fill(self, tensors, column: int):
-        """the tensors' addresses into the table (0: p, 1: g); their dtype as
-        the library numbers it, or -1 where they are not what they must be"""
-        return _native()[0](tensors, len(self.table), self.sizes, self.device.index, C.addressof(self.table) + 8 * column,
-                            _WORDS)
+    @property
+    def bits(self) -> int:
+        """32 or 8: what the moments are held in"""
+        return self._bits
 
     def _refuse(self, grads):
         """what is wrong with the tensors of a step"""
@@ -171,6 +178,15 @@ class AdamW:
                     not s.is_contiguous():
                 raise ValueError(f"state[{k!r}] must be {dt} [{n}] on {self.device}")
 
+    def _state_addresses(self):
+        """where the state's tensors lie now, in their order"""
+        tensors, dev = [self.state.get(k) for k in self._names], self.device
+        if dev.type != "cuda" or not _native()[2](tensors, len(tensors), self._lengths, self._types, dev.index, self._at):
+            self._check_state()
+            tc._need_gpu(*tensors)
+            raise ValueError("state: dense tensors with memory of their own are needed")
+        return self._at
+
     def step(self, grads=None, clip: torch.Tensor = None):
         """one step.  grads: a tensor per parameter (of one dtype), else their
         .grad; clip: what grad_norm returned, else the gradients as they are.
@@ -184,30 +200,29 @@ class AdamW:
             raise ValueError(f"clip must be float32 [2] on {dev}")
         if dev.type == "cuda" and torch.cuda.is_current_stream_capturing():
             raise RuntimeError("a captured step would repeat its number and seed at every replay")
-        gdt = self._fill(grads, 1) if dev.type == "cuda" else -1
-        if gdt < 0 or self._fill(self.params, 0) != tc._DT[self.dtype]:
-            self._refuse(grads)
-        st = self.state
-        if st["m"].numel() != self.size or st["v"].numel() != self.size:
+        # (all of them may have been replaced, or changed their memory, since they were looked at last)
+        state, at = [self.state.get(k) for k in self._names], self._at
+        dts = _native()[0](self.params, grads, len(self.table), self.sizes, C.addressof(self.table), _WORDS, state,
+                           len(state), self._lengths, self._types, at, dev.index) if dev.type == "cuda" else -1
+        if dts & 3 != tc._DT[self.dtype]:
             self._check_state()
+            self._refuse(grads)
         t = self.t + 1
         a = tc.AdamwSettings(self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay, t, self.bits,
-                             (self.seed + 1) & 0x7FFFFFFF, st["m"].data_ptr(), st["v"].data_ptr(),
-                             tc._ptr(st.get("em")), tc._ptr(st.get("ev")))
-        tc._check(tc.lib().tc_adamw_step(C.byref(a), self.table, len(self.table), tc._DT[self.dtype], gdt,
+                             (self.seed + 1) & 0x7FFFFFFF, *at)
+        tc._check(tc.lib().tc_adamw_step(C.byref(a), self.table, len(self.table), dts & 3, dts >> 2,
                                          tc._ptr(clip), tc._stream(dev)), "tc_adamw_step")
         self.t, self.seed = t, (self.seed + 1) & 0x7FFFFFFF
 
     def moments(self):
         """(m, v) as float32 [positions]: the state itself, or the values that
         its codes stand for"""
-        st = self.state
         if self.bits == 32:
-            return st["m"], st["v"]
+            self._check_state()
+            return self.state["m"], self.state["v"]
+        am, av, aem, aev = self._state_addresses()
         m = torch.empty(self.size, dtype=torch.float32, device=self.device)
         v = torch.empty(self.size, dtype=torch.float32, device=self.device)
-        tc._need_gpu(m)
-        tc._check(tc.lib().tc_adamw_moments(st["m"].data_ptr(), st["em"].data_ptr(), st["v"].data_ptr(),
-                                            st["ev"].data_ptr(), self.size, m.data_ptr(), v.data_ptr(),
+        tc._check(tc.lib().tc_adamw_moments(am, aem, av, aev, self.size, m.data_ptr(), v.data_ptr(),
                                             tc._stream(self.device)), "tc_adamw_moments")
         return m, v

@@ -279,3 +279,36 @@ def test_a_step_is_not_captured(optim):
     assert opt.t == 0 and torch.equal(ps[0], before)
     opt.step(gs)
     assert opt.t == 1 and not torch.equal(ps[0], before)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_replaced_states(optim, bits):
+    """good ones are taken, whatever the object; others are refused before the launch"""
+    ps, _, _ = views([300, 70], torch.float32, 0, 32)
+    gs, _, _ = views([300, 70], torch.float32, 0, 33)
+    qs = [p.clone() for p in ps]
+    a, b = optim.AdamW(ps, state_bits=bits, **HP), optim.AdamW(qs, state_bits=bits, **HP)
+    a.step(gs)
+    b.step(gs)
+    a.state = {k: s.clone() for k, s in a.state.items()}
+    a.state["m"].data = a.state["m"].clone()
+    a.step(gs)
+    b.step(gs)
+    for p, q in zip(ps, qs):
+        assert torch.equal(p, q)
+    good, before = a.state, [p.clone() for p in ps]
+    for k in good:
+        for wrong in (good[k].cpu(), good[k].to(torch.float16), good[k][1:], good[k].view(1, -1), torch.cat([good[k], good[k]])[::2], None):
+            a.state = {**good, k: wrong}
+            with pytest.raises(ValueError, match="state"):
+                a.step(gs)
+            with pytest.raises(ValueError, match="state"):
+                a.moments()
+    a.state = dict(good)
+    a.state["m"] = good["m"].clone()
+    a.state["m"].data = torch.zeros(3, device="cuda")
+    with pytest.raises(ValueError, match="state"):
+        a.step(gs)
+    assert a.t == 2
+    for p, q in zip(ps, before):
+        assert torch.equal(p, q)

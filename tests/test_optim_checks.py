@@ -142,3 +142,45 @@ def test_norm_refusals():
     assert L.tc_grad_norm(C.byref(t), 1, 0, 1.0, out, ws + 4, need, None) == tc.TC_ERR_ALIGN
     bad = row(g=BASE + 2)
     assert L.tc_grad_norm(C.byref(bad), 1, 0, 1.0, out, ws, need, None) == tc.TC_ERR_ALIGN
+
+
+WRONG_STATES = {
+    "other dtype": lambda s: {**s, "m": s["m"].to(torch.float16)},
+    "other size": lambda s: {**s, "v": s["v"][:-1]},
+    "strided": lambda s: {**s, "m": torch.zeros(2 * s["m"].numel(), dtype=s["m"].dtype, device=s["m"].device)[::2]},
+    "two dimensions": lambda s: {**s, "v": s["v"].view(2, -1)},
+    "other device": lambda s: {**s, "m": torch.zeros_like(s["m"], device="meta")},
+    "missing": lambda s: {k: t for k, t in s.items() if k != "v"},
+    "none": lambda s: {**s, "m": None},
+    "short exponents": lambda s: {**s, "em": s["em"][:0]},
+    "wide exponents": lambda s: {**s, "ev": s["ev"].to(torch.int32)},
+}
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("what", list(WRONG_STATES))
+@pytest.mark.parametrize("same_object", [True, False])
+def test_a_replaced_state_is_looked_at(what, bits, same_object):
+    """the state is a public attribute: what a step finds there is checked every time, before anything is launched"""
+    if bits == 32 and "exponents" in what:
+        pytest.skip("binary32 moments have none")
+    p = torch.zeros(300)
+    o = optim.AdamW([p], lr=1.0, state_bits=bits)
+    wrong = WRONG_STATES[what](o.state)
+    if same_object:
+        o.state.clear()
+        o.state.update(wrong)
+    else:
+        o.state = wrong
+    with pytest.raises(ValueError, match="state"):
+        o.step([torch.zeros(300)])
+    with pytest.raises(ValueError, match="state"):
+        o.moments()
+    assert o.t == 0
+
+
+def test_the_width_of_the_moments_is_fixed():
+    o = optim.AdamW([torch.zeros(300)], lr=1.0, state_bits=8)
+    assert o.bits == 8
+    with pytest.raises(AttributeError):
+        o.bits = 32
