@@ -312,3 +312,26 @@ def test_replaced_states(optim, bits):
     assert a.t == 2
     for p, q in zip(ps, before):
         assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("pdt,gdt", [("f32", "bf16"), ("bf16", "f32"), ("bf16", "f16"), ("f16", "bf16"), ("f16", "f16")])
+def test_adamw_8_other_types(optim, pdt, gdt):
+    """the type pairs of 8-bit moments that the bit by bit test leaves out: moments as of the same gradients in
+    binary32 (exactly), parameters by the formula"""
+    ps, pflat, pgap = views(SIZES, DT[pdt], 1, 34)
+    qs = [p.float().clone() for p in ps]
+    a, b = optim.AdamW(ps, state_bits=8, seed=7, **HP), optim.AdamW(qs, state_bits=8, seed=7, **HP)
+    clip = torch.tensor([2.0, 0.25], device="cuda")
+    for t in (1, 2):
+        gs, _, _ = views(SIZES, DT[gdt], 1, 40 + t, 0.1)
+        m0, v0 = (np64(x) for x in a.moments())
+        p0 = [np64(p) for p in ps]
+        a.step(gs, clip=clip)
+        b.step([g.float() for g in gs], clip=clip)
+        for k in a.state:
+            assert torch.equal(a.state[k], b.state[k])
+        for p, g, q0, at in zip(ps, gs, p0, a.places):
+            s = slice(at, at + p.numel())
+            w, _, _ = R.adamw64(q0, np64(g), m0[s], v0[s], 0.25, HP["lr"], *HP["betas"], HP["eps"], HP["weight_decay"], t)
+            check_p(np64(p), w, q0, w - q0 * (1 - HP["lr"] * HP["weight_decay"]), pdt)
+    assert bool((pflat[pgap] == 7.0).all())
