@@ -109,13 +109,16 @@ class AdamW:
 
     state_bits  32: binary32 moments; 8: codes with an exponent per 256 positions
     master      keep the parameters in binary32 beside 16-bit ones, which
-                receive their rounding
-    state       moments to go on from (as `state` holds them), else zeros
+                receive their rounding: state["w32"], and w32[k] for tensor k
+    state       what to go on from (as `state` holds it), else moments of zero.
+                Masters that it does not hold start from the parameters
     t, seed     steps taken so far, and the seed of 8-bit rounding (the
                 step's number is added to it)
 
-    Positions: each tensor's moments start at a multiple of 256 in the flat
-    arrays `state["m"]` and `state["v"]`; places[k] is tensor k's first."""
+    A run goes on as if it had not stopped from its parameters, state, t and
+    seed.  Positions: each tensor's moments start at a multiple of 256 in the
+    flat arrays `state["m"]`, `state["v"]` and `state["w32"]`; places[k] is
+    tensor k's first."""
 
     def __init__(self, params, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
                  state_bits: int = 32, master: bool = False, state: dict = None, t: int = 0, seed: int = 0):
@@ -132,20 +135,33 @@ class AdamW:
             self.places.append(size)
             size += -(-n // BLOCK) * BLOCK
         self.size = size
+        self._master = master and self.dtype != torch.float32
         spec = self._spec()
         self._names, self._at = tuple(spec), (C.c_uint64 * len(spec))()
         self._lengths = (C.c_int64 * len(spec))(*(n for n, _ in spec.values()))
         self._types = (C.c_int8 * len(spec))(*(_STATE_TYPES[dt] for _, dt in spec.values()))
-        self.state = state if state is not None else self._zeros()
+        self.state = state if state is not None else {k: torch.zeros(n, dtype=dt, device=self.device)
+                                                      for k, (n, dt) in spec.items() if k != "w32"}
+        if not self._master and "w32" in self.state:
+            raise ValueError("state holds masters ('w32') and this optimizer keeps none")
+        if self._master and "w32" not in self.state:
+            self.state = {**self.state, "w32": torch.zeros(size, dtype=torch.float32, device=self.device)}
+            for w, p in zip(self.w32, self.params):
+                w.copy_(p.detach())
         self._check_state()
-        self.w32 = [p.detach().float() for p in self.params] if master and self.dtype != torch.float32 else None
-        for row, w in zip(self.table, self.w32 or ()):
-            row.w32 = w.data_ptr()
+        self._w32_at = 0
 
     @property
     def bits(self) -> int:
         """32 or 8: what the moments are held in"""
         return self._bits
+
+    @property
+    def w32(self):
+        """the masters, a view of the state for each tensor (None: there are none)"""
+        if not self._master:
+            return None
+        return [self.state["w32"][a:a + p.numel()].view(p.shape) for a, p in zip(self.places, self.params)]
 
     def _refuse(self, grads):
         """what is wrong with the tensors of a step"""
@@ -162,14 +178,15 @@ class AdamW:
         raise ValueError("a parameter changed its dtype, device or size")
 
     def _spec(self):
+        blocks, spec = self.size // BLOCK, {}
         if self.bits == 32:
-            return {"m": (self.size, torch.float32), "v": (self.size, torch.float32)}
-        blocks = self.size // BLOCK
-        return {"m": (self.size, torch.uint8), "v": (self.size, torch.uint8),
-                "em": (blocks, torch.int8), "ev": (blocks, torch.int8)}
-
-    def _zeros(self):
-        return {k: torch.zeros(n, dtype=dt, device=self.device) for k, (n, dt) in self._spec().items()}
+            spec.update(m=(self.size, torch.float32), v=(self.size, torch.float32))
+        else:
+            spec.update(m=(self.size, torch.uint8), v=(self.size, torch.uint8),
+                        em=(blocks, torch.int8), ev=(blocks, torch.int8))
+        if self._master:
+            spec["w32"] = (self.size, torch.float32)
+        return spec
 
     def _check_state(self):
         for k, (n, dt) in self._spec().items():
@@ -207,9 +224,13 @@ class AdamW:
         if dts & 3 != tc._DT[self.dtype]:
             self._check_state()
             self._refuse(grads)
+        if self._master and at[-1] != self._w32_at:
+            self._w32_at = at[-1]
+            for row in self.table:
+                row.w32 = at[-1] + 4 * row.pos
         t = self.t + 1
         a = tc.AdamwSettings(self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay, t, self.bits,
-                             (self.seed + 1) & 0x7FFFFFFF, *at)
+                             (self.seed + 1) & 0x7FFFFFFF, *at[:4 if self.bits == 8 else 2])
         tc._check(tc.lib().tc_adamw_step(C.byref(a), self.table, len(self.table), dts & 3, dts >> 2,
                                          tc._ptr(clip), tc._stream(dev)), "tc_adamw_step")
         self.t, self.seed = t, (self.seed + 1) & 0x7FFFFFFF
@@ -220,7 +241,7 @@ class AdamW:
         if self.bits == 32:
             self._check_state()
             return self.state["m"], self.state["v"]
-        am, av, aem, aev = self._state_addresses()
+        am, av, aem, aev = self._state_addresses()[:4]
         m = torch.empty(self.size, dtype=torch.float32, device=self.device)
         v = torch.empty(self.size, dtype=torch.float32, device=self.device)
         tc._check(tc.lib().tc_adamw_moments(am, aem, av, aev, self.size, m.data_ptr(), v.data_ptr(),

@@ -335,3 +335,34 @@ def test_adamw_8_other_types(optim, pdt, gdt):
             w, _, _ = R.adamw64(q0, np64(g), m0[s], v0[s], 0.25, HP["lr"], *HP["betas"], HP["eps"], HP["weight_decay"], t)
             check_p(np64(p), w, q0, w - q0 * (1 - HP["lr"] * HP["weight_decay"]), pdt)
     assert bool((pflat[pgap] == 7.0).all())
+
+
+@pytest.mark.parametrize("pdt", ["bf16", "f16"])
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("replace", [False, True])
+def test_a_resumed_run_goes_on_as_if_it_had_not_stopped(optim, pdt, bits, replace):
+    """parameters, state, t and seed are all of it, the binary32 masters too"""
+    ps, _, _ = views(SIZES, DT[pdt], 0, 50)
+    a = optim.AdamW(ps, state_bits=bits, master=True, seed=3, **HP)
+    steps = [views(SIZES, DT[pdt], 0, 51 + t, 0.1)[0] for t in range(6)]
+    for gs in steps[:3]:
+        a.step(gs)
+    saved = {k: s.clone() for k, s in a.state.items()}
+    qs = [p.clone() for p in ps]
+    if replace:
+        # into an optimizer that is there already
+        b = optim.AdamW(qs, state_bits=bits, master=True, **HP)
+        b.step(steps[5])
+        for q, p in zip(qs, ps):
+            q.copy_(p)
+        b.state, b.t, b.seed = saved, a.t, a.seed
+    else:
+        b = optim.AdamW(qs, state_bits=bits, master=True, state=saved, t=a.t, seed=a.seed, **HP)
+    for gs in steps[3:]:
+        a.step(gs)
+        b.step(gs)
+    for p, q in zip(ps, qs):
+        assert torch.equal(p, q)
+    for w, u in zip(a.w32, b.w32):
+        assert torch.equal(w, u)
+    assert any(not torch.equal(w, p.float()) for w, p in zip(a.w32, ps))

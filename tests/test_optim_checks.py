@@ -184,3 +184,24 @@ def test_the_width_of_the_moments_is_fixed():
     assert o.bits == 8
     with pytest.raises(AttributeError):
         o.bits = 32
+
+
+def test_masters_are_part_of_the_state():
+    p = torch.randn(5, 60).bfloat16()
+    o = optim.AdamW([p, p[:1].clone()], lr=1.0, master=True)
+    assert set(o.state) == {"m", "v", "w32"} and o.state["w32"].numel() == o.size == 768
+    assert o.w32[0].shape == p.shape and torch.equal(o.w32[0], p.float())
+    with pytest.raises(ValueError, match="w32"):
+        optim.AdamW([p], lr=1.0, state={k: torch.zeros(512) for k in ("m", "v", "w32")})
+    for wrong in (torch.zeros(767), torch.zeros(768, dtype=torch.bfloat16), torch.zeros(2, 384), None):
+        with pytest.raises(ValueError, match="w32"):
+            optim.AdamW([p, p[:1].clone()], lr=1.0, master=True, state={**o.state, "w32": wrong})
+        good, o.state = o.state, {**o.state, "w32": wrong}
+        with pytest.raises(ValueError, match="w32"):
+            o.step([p, p[:1]])
+        o.state = good
+    # (as states were held before the masters were part of them)
+    given = {k: torch.zeros(768) for k in ("m", "v")}
+    r = optim.AdamW([p, p[:1].clone()], lr=1.0, master=True, state=given)
+    assert torch.equal(r.w32[0], p.float()) and set(given) == {"m", "v"} and r.state["m"] is given["m"]
+    assert optim.AdamW([p.float()], lr=1.0, master=True).w32 is None
