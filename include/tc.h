@@ -377,7 +377,8 @@ tc_status tc_xent_step(const tc_xent* c, const void* x, const void* w, const int
  *   p    parameters [n] (tc_adamw_step: in-out; tc_grad_norm: unused)
  *   g    gradients [n]
  *   w32  NULL, or the parameters in binary32 [n], in-out: the step is taken on
- *        them and p receives their rounding
+ *        them and p receives their rounding.  An element of p that is not the
+ *        rounding of its w32 was set since: the step is taken on it
  *   n    elements, < 2^40; 0: the tensor is skipped
  *   pos  first position of its moments, a multiple of 256; the tensor owns
  *        the positions pos .. pos + 256 * ceil(n / 256) - 1 */

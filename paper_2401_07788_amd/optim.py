@@ -109,7 +109,9 @@ class AdamW:
 
     state_bits  32: binary32 moments; 8: codes with an exponent per 256 positions
     master      keep the parameters in binary32 beside 16-bit ones, which
-                receive their rounding: state["w32"], and w32[k] for tensor k
+                receive their rounding: state["w32"], and w32[k] for tensor k.
+                A parameter that something else has set since the last step
+                (a checkpoint copied into it) counts instead of its master
     state       what to go on from (as `state` holds it), else moments of zero.
                 Masters that it does not hold start from the parameters
     t, seed     steps taken so far, and the seed of 8-bit rounding (the

@@ -1,5 +1,7 @@
 """Gradient norm and AdamW over lists of tensors against 64-bit arithmetic and,
 for the codes of 8-bit moments, against the format's definition bit by bit."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -366,3 +368,38 @@ def test_a_resumed_run_goes_on_as_if_it_had_not_stopped(optim, pdt, bits, replac
     for w, u in zip(a.w32, b.w32):
         assert torch.equal(w, u)
     assert any(not torch.equal(w, p.float()) for w, p in zip(a.w32, ps))
+
+
+@pytest.mark.parametrize("pdt", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("how", ["in place", "data", "one element", "not a number"])
+def test_parameters_set_between_steps_count_although_there_are_masters(optim, pdt, bits, how):
+    """the next step is taken on them, not on the masters of what was there before (an element that is set to the
+    rounding of its master cannot be told from one that was not set, and keeps it)"""
+    ps = [torch.nn.Parameter(p.clone()) for p in views(SIZES, DT[pdt], 0, 60)[0]]
+    a = optim.AdamW(ps, state_bits=bits, master=True, seed=5, **HP)
+    for t in range(2):
+        a.step(views(SIZES, DT[pdt], 0, 61 + t, 0.1)[0])
+    before = [w.clone() for w in a.w32 or ps]
+    new = views(SIZES, DT[pdt], 0, 63)[0]
+    want = []
+    for p, w, n in zip(ps, before, new):
+        if how == "in place":
+            p.data.copy_(n)
+            want.append(torch.where(w.detach().to(DT[pdt]) == n, w.detach().float(), n.float()))
+        elif how == "data":
+            p.data = n.clone()
+            want.append(torch.where(w.detach().to(DT[pdt]) == n, w.detach().float(), n.float()))
+        else:
+            w = w.detach().float().clone()
+            if p.numel():
+                p.data[-1] = w[-1] = 2.5 if how == "one element" else math.nan
+            want.append(w)
+    # the same step on binary32 parameters that hold what counts
+    qs = [w.clone() for w in want]
+    b = optim.AdamW(qs, state_bits=bits, state={k: s.clone() for k, s in a.state.items() if k != "w32"}, t=a.t, seed=a.seed, **HP)
+    gs = views(SIZES, DT[pdt], 0, 64, 0.1)[0]
+    a.step(gs)
+    b.step(gs)
+    for p, w, q in zip(ps, a.w32 or ps, qs):
+        assert torch.equal(w.nan_to_num(7.0), q.nan_to_num(7.0)) and torch.equal(p.data.nan_to_num(7.0), q.to(DT[pdt]).nan_to_num(7.0))
