@@ -34,8 +34,7 @@ class Pipeline:
         self.w2, self.vocab = weight(hidden, hidden), weight(vocab, hidden)      # last stage
         self.boundary = boundary.TopkBoundary(*keep)
         opt = dict(lr=4e-3, weight_decay=0.01, state_bits=state_bits, master=True)
-        self.stages = [(ps, optim.AdamW([p.data for p in ps], **opt))
-                       for ps in ([self.embed, self.w1], [self.w2, self.vocab])]
+        self.stages = [(ps, optim.AdamW(ps, **opt)) for ps in ([self.embed, self.w1], [self.w2, self.vocab])]
 
     def step(self, tokens, target):
         """one step on tokens and their targets (PADDING: none); returns the mean loss"""

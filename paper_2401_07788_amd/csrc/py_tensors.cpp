@@ -76,6 +76,23 @@ extern "C" __attribute__((visibility("default"))) int tc_py_step(PyObject* param
   }
 }
 
+// After a step: every tensor of `list` was written in place, and autograd is
+// told (as an operation of torch's own would), so that a backward pass that
+// saved one of them before is refused.
+extern "C" __attribute__((visibility("default"))) void tc_py_written(PyObject* list) {
+  try {
+    if (!PyList_Check(list) && !PyTuple_Check(list)) return;
+    for (Py_ssize_t k = 0; k < PySequence_Fast_GET_SIZE(list); ++k) {
+      PyObject* const item = PySequence_Fast_GET_ITEM(list, k);
+      if (!THPVariable_Check(item)) continue;
+      const at::Tensor& t = THPVariable_Unpack(item);
+      // (inference tensors have no counter)
+      if (t.defined() && !t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+    }
+  } catch (...) {
+  }
+}
+
 // The table of a list that is looked at for the first time: each tensor's
 // address to table[k * stride + at] and its elements to table[k * stride + n_at]
 // and, unless NULL, to sizes[k]; its first position in the moments (multiples

@@ -23,19 +23,20 @@ _py = None
 
 
 def _native():
-    """(tc_py_step, tc_py_table, tc_py_state) of libtc_py.so (csrc/py_tensors.cpp)"""
+    """(tc_py_step, tc_py_table, tc_py_state, tc_py_written) of libtc_py.so (csrc/py_tensors.cpp)"""
     global _py
     if _py is None:
         if not os.path.exists(_PY_PATH):
             raise RuntimeError(f"{_PY_PATH} is missing: build it with paper_2401_07788_amd.build.build()")
         lib = C.PyDLL(_PY_PATH)
-        f, g, h = lib.tc_py_step, lib.tc_py_table, lib.tc_py_state
-        f.restype, g.restype, h.restype = C.c_int, C.py_object, C.c_int
+        f, g, h, w = lib.tc_py_step, lib.tc_py_table, lib.tc_py_state, lib.tc_py_written
+        f.restype, g.restype, h.restype, w.restype = C.c_int, C.py_object, C.c_int, None
         f.argtypes = [C.py_object, C.py_object, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.py_object, C.c_int64,
                       C.c_void_p, C.c_void_p, C.c_void_p, C.c_int]
         g.argtypes = [C.py_object, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_void_p]
         h.argtypes = [C.py_object, C.c_int64, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p]
-        _py = f, g, h
+        w.argtypes = [C.py_object]
+        _py = f, g, h, w
     return _py
 
 
@@ -105,7 +106,8 @@ def grad_norm(grads, max_norm: float, out: torch.Tensor = None, ws: torch.Tensor
 
 class AdamW:
     """AdamW over a stage's parameters (tensors of one dtype on one device,
-    updated in place).
+    updated in place, which autograd is told; p.data has a version counter of
+    its own, so give the parameters themselves).
 
     state_bits  32: binary32 moments; 8: codes with an exponent per 256 positions
     master      keep the parameters in binary32 beside 16-bit ones, which
@@ -235,6 +237,7 @@ class AdamW:
                              (self.seed + 1) & 0x7FFFFFFF, *at[:4 if self.bits == 8 else 2])
         tc._check(tc.lib().tc_adamw_step(C.byref(a), self.table, len(self.table), dts & 3, dts >> 2,
                                          tc._ptr(clip), tc._stream(dev)), "tc_adamw_step")
+        _native()[3](self.params)
         self.t, self.seed = t, (self.seed + 1) & 0x7FFFFFFF
 
     def moments(self):

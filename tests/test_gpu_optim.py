@@ -403,3 +403,32 @@ def test_parameters_set_between_steps_count_although_there_are_masters(optim, pd
     b.step(gs)
     for p, w, q in zip(ps, a.w32 or ps, qs):
         assert torch.equal(w.nan_to_num(7.0), q.nan_to_num(7.0)) and torch.equal(p.data.nan_to_num(7.0), q.to(DT[pdt]).nan_to_num(7.0))
+
+
+@pytest.mark.parametrize("given", ["parameter", "detached", "view"])
+def test_autograd_notices_a_step(optim, given):
+    """a backward pass through values that the step has overwritten is refused; a refused step leaves no trace"""
+    p = torch.nn.Parameter(torch.randn(8, 30, device="cuda"))
+    own = {"parameter": p, "detached": p.detach(), "view": p.detach().view(-1)}[given]
+    opt = optim.AdamW([own], **HP)
+    y = (p * p).sum()
+    version = p._version
+    with pytest.raises(ValueError):
+        opt.step([torch.zeros(3, device="cuda")])
+    assert p._version == version
+    opt.step([torch.ones_like(own)])
+    assert p._version > version
+    with pytest.raises(RuntimeError, match="inplace"):
+        y.backward()
+    (p * p).sum().backward()
+    assert torch.equal(p.grad, 2 * p.detach())
+
+
+def test_a_step_on_inference_tensors(optim):
+    with torch.inference_mode():
+        p = torch.randn(300, device="cuda")
+    q = p.clone()
+    g = torch.randn(300, device="cuda")
+    optim.AdamW([p], **HP).step([g])
+    optim.AdamW([q], **HP).step([g])
+    assert torch.equal(p, q)
