@@ -14,6 +14,7 @@ import ctypes as C
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd import forward_ad
 
 from . import tc
 
@@ -51,6 +52,13 @@ def _sizes(x, w, target, ignore_index, chunk):
         raise ValueError("x, w and target must be on one device")
     tc._need_gpu(target)
     return tc.Xent(x.shape[0], w.shape[0], x.shape[1], ldx, ldw, ignore_index, chunk, tc._dt(x), 0)
+
+
+def _no_tangent(*ts):
+    """forward-mode derivatives are not computed: refused, not taken for zero"""
+    for t in ts:
+        if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+            raise NotImplementedError("the loss has no forward-mode derivative")
 
 
 _ws_cache = {}
@@ -105,6 +113,7 @@ def linear_xent_step(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, wei
     sum(weight * loss) (weight: float32 [n], None: 1).  Rows of x and w may lie
     apart.  chunk: tokens whose softmax entries are held at once (0: as many
     as 4 GiB hold).  Tokens whose target is ignore_index do not count."""
+    _no_tangent(x, w, weight)
     c = _sizes(x, w, target, ignore_index, chunk)
     if weight is not None and (weight.dtype != torch.float32 or weight.shape != target.shape or weight.device != x.device):
         raise ValueError(f"weight must be float32 [{x.shape[0]}] on {x.device}")
@@ -146,7 +155,9 @@ class _LinearXent(torch.autograd.Function):
 
 def linear_xent(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, ignore_index: int = -100, chunk: int = 0):
     """(loss, lse), float32 [n]: the losses of the tokens x [n, h] against
-    w [v, h].  The losses are differentiable in x and w, once; lse is not."""
+    w [v, h].  The losses are differentiable in x and w, once and backward;
+    lse is not."""
+    _no_tangent(x, w)
     if torch.is_grad_enabled() and (x.requires_grad or w.requires_grad):
         return _LinearXent.apply(x, w, target, ignore_index, chunk)
     return _loss(x, w, target, ignore_index, chunk)

@@ -103,3 +103,22 @@ def test_overlapping_buffers_in_the_debug_library():
     a = [BASE + (k << 30) for k in range(9)]
     a[6] = a[0]
     assert D.tc_xent_step(C.byref(c), *a, 1 << 30, None) == tc.TC_ERR_PRECONDITION
+
+
+def test_forward_mode_is_refused():
+    """a dual tensor's derivative would else come back as none, which counts as zero"""
+    x, w, t, g = torch.zeros(4, 8), torch.zeros(5, 8), torch.zeros(4, dtype=torch.int64), torch.zeros(4)
+    with torch.autograd.forward_ad.dual_level():
+        dx, dw, dg = (torch.autograd.forward_ad.make_dual(a, torch.ones_like(a)) for a in (x, w, g))
+        for a, b in ((dx, w), (x, dw), (dx.requires_grad_(), w)):
+            with pytest.raises(NotImplementedError, match="forward-mode"):
+                head.linear_xent(a, b, t)
+            with torch.no_grad(), pytest.raises(NotImplementedError, match="forward-mode"):
+                head.linear_xent(a, b, t)
+            with pytest.raises(NotImplementedError, match="forward-mode"):
+                head.linear_xent_step(a, b, t)
+        with pytest.raises(NotImplementedError, match="forward-mode"):
+            head.linear_xent_step(x, w, t, dg)
+        # (others go on: to the refusal of tensors that are not on a GPU)
+        with pytest.raises(ValueError, match="GPU"):
+            head.linear_xent(x, w, t)
