@@ -101,9 +101,10 @@ def _loss(x, w, target, ignore_index, chunk=0, ws=None):
     loss = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
     lse = torch.empty_like(loss)
     st = tc._stream(x.device)
-    ws = _workspace(c, 0, x.device, st, ws)
-    tc._check(tc.lib().tc_xent_loss(C.byref(c), x.data_ptr(), w.data_ptr(), target.data_ptr(), loss.data_ptr(),
-                                    lse.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(), st), "tc_xent_loss")
+    with tc._stream_lock(x.device, st):
+        ws = _workspace(c, 0, x.device, st, ws)
+        tc._check(tc.lib().tc_xent_loss(C.byref(c), x.data_ptr(), w.data_ptr(), target.data_ptr(), loss.data_ptr(),
+                                        lse.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(), st), "tc_xent_loss")
     return loss, lse
 
 
@@ -129,10 +130,11 @@ def linear_xent_step(x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, wei
                 raise ValueError(f"out.{name} must be {dt} {list(s)} on {x.device}")
         tc._need_gpu(*out)
     st = tc._stream(x.device)
-    ws = _workspace(c, 1, x.device, st, ws)
-    tc._check(tc.lib().tc_xent_step(C.byref(c), x.data_ptr(), w.data_ptr(), target.data_ptr(), tc._ptr(weight),
-                                    out.loss.data_ptr(), out.lse.data_ptr(), out.dx.data_ptr(), out.dw.data_ptr(),
-                                    ws.data_ptr(), ws.numel() * ws.element_size(), st), "tc_xent_step")
+    with tc._stream_lock(x.device, st):
+        ws = _workspace(c, 1, x.device, st, ws)
+        tc._check(tc.lib().tc_xent_step(C.byref(c), x.data_ptr(), w.data_ptr(), target.data_ptr(), tc._ptr(weight),
+                                        out.loss.data_ptr(), out.lse.data_ptr(), out.dx.data_ptr(), out.dw.data_ptr(),
+                                        ws.data_ptr(), ws.numel() * ws.element_size(), st), "tc_xent_step")
     return out
 
 

@@ -95,12 +95,13 @@ def grad_norm(grads, max_norm: float, out: torch.Tensor = None, ws: torch.Tensor
     if ws is None and torch.cuda.is_current_stream_capturing():
         # a graph keeps its own: a larger call would free the stream's under it
         ws = torch.zeros(lst.ws_bytes, dtype=torch.uint8, device=lst.device)
-    if ws is None:
-        ws = tc._ws_cache.get((lst.device.index, st))
-        if ws is None or ws.numel() < lst.ws_bytes:
-            ws = tc._workspace_of(lst.ws_bytes, lst.device)
-    tc._check(tc.lib().tc_grad_norm(lst.table, len(lst.table), tc._DT[lst.dtype], max_norm, out.data_ptr(),
-                                    ws.data_ptr(), ws.numel() * ws.element_size(), st), "tc_grad_norm")
+    with tc._stream_lock(lst.device, st):
+        if ws is None:
+            ws = tc._ws_cache.get((lst.device.index, st))
+            if ws is None or ws.numel() < lst.ws_bytes:
+                ws = tc._workspace_of(lst.ws_bytes, lst.device)
+        tc._check(tc.lib().tc_grad_norm(lst.table, len(lst.table), tc._DT[lst.dtype], max_norm, out.data_ptr(),
+                                        ws.data_ptr(), ws.numel() * ws.element_size(), st), "tc_grad_norm")
     return out
 
 

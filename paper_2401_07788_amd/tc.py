@@ -303,6 +303,18 @@ def _workspace_of(n: int, device) -> torch.Tensor:
     return ws
 
 
+_stream_locks = {}
+
+
+def _stream_lock(device, stream):
+    """held by a call from looking up its stream's workspace until its last
+    launch is out: the foreign call releases the interpreter's lock, and the
+    launches of a call in another thread on the same stream (one thread's
+    forward pass beside another's backward pass) would fall between its own"""
+    key = (device.index, stream)
+    return _stream_locks.get(key) or _stream_locks.setdefault(key, threading.RLock())
+
+
 def device_errors(clear: bool = True) -> int:
     """sticky TC_KERR_* bits of the current device (synchronizes it).  After a
     timed-out cross-workgroup wait the cached workspaces are zero-filled again."""

@@ -1,0 +1,82 @@
+"""Host threads on one stream: a call's launches, all of which use the stream's
+one workspace, are not interrupted by another call's.  The foreign calls are
+replaced here by ones that wait for a second one to enter (a foreign call
+releases the interpreter's lock, so a second thread may); no GPU is used."""
+import ctypes as C
+import threading
+import types
+
+import pytest
+import torch
+
+from paper_2401_07788_amd import head, optim, tc
+
+
+class Library:
+    """stands for the library: a call stays until another one enters the same workspace, or for a moment"""
+
+    def __init__(self):
+        self.inside, self.met, self.calls, self.lock = [], False, [], threading.Condition()
+
+    def launch(self, name, ws):
+        with self.lock:
+            if ws in self.inside:
+                self.met = True
+            self.inside.append(ws)
+            self.calls.append(name)
+            self.lock.notify_all()
+            self.lock.wait_for(lambda: self.met, timeout=0.3)
+            self.inside.remove(ws)
+        return 0
+
+    def tc_xent_workspace_bytes(self, c, grad, n):
+        C.cast(n, C.POINTER(C.c_size_t))[0] = 5000
+        return 0
+
+    def tc_xent_loss(self, *a):
+        return self.launch("loss", a[-3])
+
+    def tc_xent_step(self, *a):
+        return self.launch("step", a[-3])
+
+    def tc_grad_norm_workspace_bytes(self, n):
+        return 5000
+
+    def tc_grad_norm(self, *a):
+        return self.launch("norm", a[-3])
+
+
+@pytest.fixture
+def library(monkeypatch):
+    lib = Library()
+    monkeypatch.setattr(tc, "lib", lambda: lib)
+    monkeypatch.setattr(tc, "_need_gpu", lambda *ts: None)
+    monkeypatch.setattr(tc, "_stream", lambda device: 0)
+    monkeypatch.setattr(tc, "_ws_cache", {})
+    monkeypatch.setattr(head, "_ws_cache", {})
+    monkeypatch.setattr(head, "_ws_bytes", {})
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: types.SimpleNamespace(cuda_stream=0))
+    return lib
+
+
+X, W, T = torch.zeros(4, 8), torch.zeros(5, 8), torch.zeros(4, dtype=torch.int64)
+G = [torch.zeros(10), torch.zeros(3)]
+CALLS = {
+    "loss": lambda: head.linear_xent(X, W, T),
+    "step": lambda: head.linear_xent_step(X, W, T),
+    "norm": lambda: optim.grad_norm(G, 1.0),
+}
+
+
+@pytest.mark.parametrize("first,second", [("loss", "loss"), ("step", "step"), ("loss", "step"), ("norm", "norm")])
+def test_calls_on_one_stream_take_turns(library, first, second):
+    CALLS[first](), CALLS[second]()              # (the stream has its workspace)
+    library.calls.clear()
+    threads = [threading.Thread(target=CALLS[c]) for c in (first, second)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert sorted(library.calls) == sorted([first, second])
+    assert not library.met

@@ -489,3 +489,23 @@ def test_binary32_token_of_zeros_among_large_ones(head):
             # d and w as pairs of binary16 (22 bits each), 100 products summed
             lim = (2.0 ** -20 + 2.0 ** -17) * (d.abs() @ w.double().abs())
             assert bool(((r.dx[7].double() - d @ w.double()).abs() <= lim).all())
+
+
+def test_two_threads_on_one_stream(head):
+    """forward passes of one thread beside another's steps: each gets what it gets alone"""
+    import threading
+    a, b = inputs(150, 700, 64, "bf16", 30), inputs(300, 500, 96, "bf16", 31)
+    want_a, want_b = head.linear_xent_step(*a), head.linear_xent(*b)
+    torch.cuda.synchronize()
+    got_a, got_b = [], []
+    threads = [threading.Thread(target=lambda: got_a.extend(head.linear_xent_step(*a) for _ in range(40))),
+               threading.Thread(target=lambda: got_b.extend(head.linear_xent(*b) for _ in range(80)))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert len(got_a) == 40 and len(got_b) == 80
+    for got, want in [(g, want_a) for g in got_a] + [(g, want_b) for g in got_b]:
+        for p, q in zip(got, want):
+            assert torch.equal(p, q)
