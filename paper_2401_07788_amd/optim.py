@@ -82,6 +82,11 @@ class TensorList:
         self.ws_bytes = int(tc.lib().tc_grad_norm_workspace_bytes(len(self.tensors)))
 
 
+# by device and stream, zero between calls: not the boundary's, which graphs may
+# hold and which a longer list would replace by a larger one
+_ws_cache = {}
+
+
 def grad_norm(grads, max_norm: float, out: torch.Tensor = None, ws: torch.Tensor = None) -> torch.Tensor:
     """float32 [2]: the norm over all tensors of `grads` (a TensorList or
     tensors), and min(1, max_norm / (norm + 1e-6)), the factor that clips them"""
@@ -97,9 +102,9 @@ def grad_norm(grads, max_norm: float, out: torch.Tensor = None, ws: torch.Tensor
         ws = torch.zeros(lst.ws_bytes, dtype=torch.uint8, device=lst.device)
     with tc._stream_lock(lst.device, st):
         if ws is None:
-            ws = tc._ws_cache.get((lst.device.index, st))
+            ws = _ws_cache.get((lst.device.index, st))
             if ws is None or ws.numel() < lst.ws_bytes:
-                ws = tc._workspace_of(lst.ws_bytes, lst.device)
+                ws = _ws_cache[(lst.device.index, st)] = torch.zeros(lst.ws_bytes, dtype=torch.uint8, device=lst.device)
         tc._check(tc.lib().tc_grad_norm(lst.table, len(lst.table), tc._DT[lst.dtype], max_norm, out.data_ptr(),
                                         ws.data_ptr(), ws.numel() * ws.element_size(), st), "tc_grad_norm")
     return out

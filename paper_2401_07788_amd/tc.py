@@ -291,10 +291,8 @@ def workspace(c: Codec, device=None) -> torch.Tensor | None:
     and stream (every completed call leaves it zero-filled again)"""
     device = torch.device(device or torch.cuda.current_device())
     n = workspace_bytes(c)
-    return None if n == 0 else _workspace_of(n, device)
-
-
-def _workspace_of(n: int, device) -> torch.Tensor:
+    if n == 0:
+        return None
     key = (device.index, torch.cuda.current_stream(device).cuda_stream)
     ws = _ws_cache.get(key)
     if ws is None or ws.numel() < n:

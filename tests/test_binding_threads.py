@@ -54,6 +54,7 @@ def library(monkeypatch):
     monkeypatch.setattr(tc, "_stream", lambda device: 0)
     monkeypatch.setattr(tc, "_ws_cache", {})
     monkeypatch.setattr(head, "_ws_cache", {})
+    monkeypatch.setattr(optim, "_ws_cache", {}, raising=False)
     monkeypatch.setattr(head, "_ws_bytes", {})
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: types.SimpleNamespace(cuda_stream=0))
@@ -79,4 +80,15 @@ def test_calls_on_one_stream_take_turns(library, first, second):
     for t in threads:
         t.join()
     assert sorted(library.calls) == sorted([first, second])
+    assert not library.met
+
+
+def test_the_norm_leaves_the_boundarys_workspace_alone(library):
+    """a graph may hold that of a boundary call; a longer list of gradients does not replace it"""
+    small = tc._ws_cache[(None, 0)] = torch.zeros(100, dtype=torch.uint8)
+    optim.grad_norm(G, 1.0)
+    assert tc._ws_cache == {(None, 0): small}
+    large = tc._ws_cache[(None, 0)] = torch.zeros(1 << 20, dtype=torch.uint8)
+    library.inside.append(large.data_ptr())
+    optim.grad_norm(G, 1.0)
     assert not library.met

@@ -432,3 +432,31 @@ def test_a_step_on_inference_tensors(optim):
     optim.AdamW([p], **HP).step([g])
     optim.AdamW([q], **HP).step([g])
     assert torch.equal(p, q)
+
+
+def test_a_graph_of_the_boundary_keeps_its_workspace(optim, tc):
+    """a norm over many tensors on the same stream, between the replays, does not take it away"""
+    x = torch.randn(1, 40000, device="cuda")
+    xs, out = x.clone(), tc.empty_topk_payload(1, 40000, 4000, torch.float32, "cuda")
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        tc.topk_compress(xs, 4000, 1, out=out)
+    side.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        tc.topk_compress(xs, 4000, 1, out=out)
+    gs = views([3] * 4000, torch.float32, 0, 70)[0]
+    for k in range(3):
+        xs.copy_(x * (k + 1.5) + k)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            optim.grad_norm(gs, 1.0)
+            filler = torch.full((64 << 20,), 255, dtype=torch.uint8, device="cuda")
+        side.synchronize()
+        want = tc.topk_compress(xs, 4000, 1)
+        graph.replay()
+        torch.cuda.synchronize()
+        del filler
+        for p, q in zip(out, want):
+            assert torch.equal(p, q)
+    assert tc.device_errors() == 0
