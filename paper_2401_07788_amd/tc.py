@@ -358,9 +358,10 @@ def topk_compress(x: torch.Tensor, k: int, n_seg: int, ws=None, out: TopkPayload
         out = empty_topk_payload(n_seg, L, k, x.dtype, x.device, blk)
     p = Payload(_ptr(out.idx), _ptr(out.val), None, None, _ptr(out.blk))
     st = _stream(x.device)
-    w, wn = _ws_args(c, x.device, ws, st)
-    _check(lib().tc_topk_compress(c.ref, _ptr(x), _dt(x), C.byref(p), w, wn, st),
-           "tc_topk_compress")
+    with _stream_lock(x.device, st):
+        w, wn = _ws_args(c, x.device, ws, st)
+        _check(lib().tc_topk_compress(c.ref, _ptr(x), _dt(x), C.byref(p), w, wn, st),
+               "tc_topk_compress")
     return out
 
 
@@ -418,8 +419,9 @@ def quant_pack(x: torch.Tensor, bits: int, n_grp: int, ws=None):
     meta = torch.empty((n_grp, 2), dtype=torch.float32, device=x.device)
     p = Payload(None, None, _ptr(codes), _ptr(meta), None)
     st = _stream(x.device)
-    w, wn = _ws_args(c, x.device, ws, st)
-    _check(lib().tc_quant_pack(c.ref, _ptr(x), _dt(x), C.byref(p), w, wn, st), "tc_quant_pack")
+    with _stream_lock(x.device, st):
+        w, wn = _ws_args(c, x.device, ws, st)
+        _check(lib().tc_quant_pack(c.ref, _ptr(x), _dt(x), C.byref(p), w, wn, st), "tc_quant_pack")
     return codes, meta
 
 
@@ -459,9 +461,10 @@ def ef_step_topk(x: torch.Tensor, e: torch.Tensor, k: int, n_seg: int, ws=None, 
         out = empty_topk_payload(n_seg, L, k, x.dtype, x.device, blk)
     p = Payload(_ptr(out.idx), _ptr(out.val), None, None, _ptr(out.blk))
     st = _stream(x.device)
-    w, wn = _ws_args(c, x.device, ws, st)
-    _check(lib().tc_ef_step(c.ref, _ptr(x), _dt(x), e.data_ptr(), C.byref(p),
-                            w, wn, st), "tc_ef_step")
+    with _stream_lock(x.device, st):
+        w, wn = _ws_args(c, x.device, ws, st)
+        _check(lib().tc_ef_step(c.ref, _ptr(x), _dt(x), e.data_ptr(), C.byref(p),
+                                w, wn, st), "tc_ef_step")
     return out
 
 
@@ -483,9 +486,10 @@ def ef_step_quant(x: torch.Tensor, e: torch.Tensor, bits: int, n_grp: int, ws=No
         meta = torch.empty((n_grp, 2), dtype=torch.float32, device=x.device)
     p = Payload(None, None, _ptr(codes), _ptr(meta), None)
     st = _stream(x.device)
-    w, wn = _ws_args(c, x.device, ws, st)
-    _check(lib().tc_ef_step(c.ref, _ptr(x), _dt(x), e.data_ptr(), C.byref(p),
-                            w, wn, st), "tc_ef_step")
+    with _stream_lock(x.device, st):
+        w, wn = _ws_args(c, x.device, ws, st)
+        _check(lib().tc_ef_step(c.ref, _ptr(x), _dt(x), e.data_ptr(), C.byref(p),
+                                w, wn, st), "tc_ef_step")
     return codes, meta
 
 
@@ -539,9 +543,10 @@ def ef_step_topk_quant(x: torch.Tensor, e: torch.Tensor, k: int, bits: int, n_se
         out = empty_topk_quant_payload(n_seg, L, k, bits, dev, blk)
     p = Payload(_ptr(out.idx), None, _ptr(out.codes), _ptr(out.meta), _ptr(out.blk))
     st = _stream(dev)
-    w, wn = _ws_args(c, dev, ws, st)
-    _check(lib().tc_ef_step(c.ref, _ptr(x), _dt(x), e.data_ptr(), C.byref(p),
-                            w, wn, st), "tc_ef_step")
+    with _stream_lock(dev, st):
+        w, wn = _ws_args(c, dev, ws, st)
+        _check(lib().tc_ef_step(c.ref, _ptr(x), _dt(x), e.data_ptr(), C.byref(p),
+                                w, wn, st), "tc_ef_step")
     return out
 
 
@@ -650,9 +655,10 @@ def aqsgd_step(a: torch.Tensor, m: torch.Tensor, ids: torch.Tensor, k: int, ws=N
     """sender: d = a - m[ids]; send TopK(d); m[ids] += sent.  m is updated in place."""
     c, n_ids, out, p = _aqsgd_prepare(a, m, ids, k, out, blk)
     st = _stream(a.device)
-    w, wn = _ws_args(c, a.device, ws, st)
-    _check(lib().tc_aqsgd_step(c.ref, _ptr(a), _dt(a), _ptr(m), m.shape[0], _ptr(ids), n_ids, C.byref(p),
-                               w, wn, st), "tc_aqsgd_step")
+    with _stream_lock(a.device, st):
+        w, wn = _ws_args(c, a.device, ws, st)
+        _check(lib().tc_aqsgd_step(c.ref, _ptr(a), _dt(a), _ptr(m), m.shape[0], _ptr(ids), n_ids, C.byref(p),
+                                   w, wn, st), "tc_aqsgd_step")
     return out
 
 

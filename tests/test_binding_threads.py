@@ -45,6 +45,18 @@ class Library:
     def tc_grad_norm(self, *a):
         return self.launch("norm", a[-3])
 
+    def tc_workspace_bytes(self, c, n):
+        C.cast(n, C.POINTER(C.c_size_t))[0] = 5000
+        return 0
+
+    def tc_quant_group_bytes(self, length, bits):
+        return length
+
+    def __getattr__(self, name):
+        if name not in ("tc_topk_compress", "tc_quant_pack", "tc_ef_step", "tc_aqsgd_step"):
+            raise AttributeError(name)
+        return lambda *a: self.launch(name, a[-3])
+
 
 @pytest.fixture
 def library(monkeypatch):
@@ -55,6 +67,7 @@ def library(monkeypatch):
     monkeypatch.setattr(tc, "_ws_cache", {})
     monkeypatch.setattr(head, "_ws_cache", {})
     monkeypatch.setattr(optim, "_ws_cache", {}, raising=False)
+    monkeypatch.setattr(tc, "_plans", {})
     monkeypatch.setattr(head, "_ws_bytes", {})
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: types.SimpleNamespace(cuda_stream=0))
@@ -62,15 +75,23 @@ def library(monkeypatch):
 
 
 X, W, T = torch.zeros(4, 8), torch.zeros(5, 8), torch.zeros(4, dtype=torch.int64)
+E = torch.zeros(4, 8)
 G = [torch.zeros(10), torch.zeros(3)]
 CALLS = {
     "loss": lambda: head.linear_xent(X, W, T),
     "step": lambda: head.linear_xent_step(X, W, T),
     "norm": lambda: optim.grad_norm(G, 1.0),
+    "tc_topk_compress": lambda: tc.topk_compress(X, 2, 4),
+    "tc_quant_pack": lambda: tc.quant_pack(X, 4, 4),
+    "tc_ef_step": lambda: tc.ef_step_topk(X, E, 2, 4),
+    "tc_ef_step ": lambda: tc.ef_step_quant(X, E, 4, 4),
+    "tc_ef_step  ": lambda: tc.ef_step_topk_quant(X, E, 2, 4, 4),
+    "tc_aqsgd_step": lambda: tc.aqsgd_step(X, E, T, 2),
 }
 
 
-@pytest.mark.parametrize("first,second", [("loss", "loss"), ("step", "step"), ("loss", "step"), ("norm", "norm")])
+@pytest.mark.parametrize("first,second", [("loss", "loss"), ("step", "step"), ("loss", "step"), ("norm", "norm"),
+                                          *((c, "tc_topk_compress") for c in CALLS if c.startswith("tc_"))])
 def test_calls_on_one_stream_take_turns(library, first, second):
     CALLS[first](), CALLS[second]()              # (the stream has its workspace)
     library.calls.clear()
@@ -79,7 +100,7 @@ def test_calls_on_one_stream_take_turns(library, first, second):
         t.start()
     for t in threads:
         t.join()
-    assert sorted(library.calls) == sorted([first, second])
+    assert sorted(library.calls) == sorted([first.strip(), second])
     assert not library.met
 
 
