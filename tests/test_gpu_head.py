@@ -509,3 +509,84 @@ def test_two_threads_on_one_stream(head):
     for got, want in [(g, want_a) for g in got_a] + [(g, want_b) for g in got_b]:
         for p, q in zip(got, want):
             assert torch.equal(p, q)
+
+
+def check_large(r, x, w, t, weight, dt):
+    """check() for sizes whose reference is better made on the device, in 64 bits and a part of the tokens at a time"""
+    n, (v, h) = x.shape[0], w.shape
+    wd, g = w.double(), torch.ones(n, device="cuda") if weight is None else weight
+    keep, top = (t >= 0) & (t < v), float(g.abs().max())
+    uz = (4 * math.sqrt(h) + 8) * 2.0 ** -24 + (2.0 ** -20 if dt == "f32" else 0)
+    low, floor = (2.0 ** -38 if dt != "bf16" else 2.0 ** -126), (2.0 ** -24 if dt == "f16" else 1e-38)
+    dw, size, worst = torch.zeros(v, h, dtype=torch.float64, device="cuda"), torch.zeros(v, h, dtype=torch.float64, device="cuda"), 0.0
+    grads = hasattr(r, "dx")
+    sums = lambda terms: 4 * math.sqrt(terms) * 2.0 ** -24             # (a product's sum, as a random walk, four deviations)
+    spread = wd.abs().sum(0)
+    for i in range(0, n, 512):
+        s = slice(i, i + 512)
+        kept, xd = keep[s], x[s].double()
+        td, gd = torch.where(kept, t[s], 0)[:, None], torch.where(kept, g[s], 0.0).double()[:, None]
+        z = xd @ wd.t().contiguous()
+        lse = torch.logsumexp(z, 1)
+        loss = lse - z.gather(1, td)[:, 0]
+        ez = uz * (xd.abs() @ wd.abs().t().contiguous()).amax(1)
+        worst = max(worst, float(ez.max()))
+        lim = 2 * ez + 2.0 ** -19 + 2.0 ** -22 * (lse.abs() + loss.abs())
+        for got, want in ((r.loss[s], loss), (r.lse[s], lse)):
+            assert bool(((got.double() - want).abs() <= lim)[kept].all()) and bool((got[~kept] == 0).all()), i
+        if not grads:
+            continue
+        p = torch.exp(z - lse[:, None])
+        hot = torch.zeros_like(p).scatter_(1, td, 1.0)
+        d, big = gd * (p - hot), gd.abs() * (p + hot)
+        rel = UD[dt] + 3 * float(ez.max()) + 2.0 ** -18 + sums(v)
+        want = d @ wd
+        lim = rel * (big @ wd.abs()) + U[dt] * want.abs() + floor + 2 * low * gd.abs() * spread
+        assert bool(((r.dx[s].double() - want).abs() <= lim).all()), ("dx", i)
+        dw += d.t().contiguous() @ xd
+        size += big.t().contiguous() @ xd.abs()
+    if grads:
+        rel = UD[dt] + 3 * worst + 2.0 ** -18 + sums(n)
+        lim = rel * size + U[dt] * dw.abs() + floor + 2 * low * top * x.double().abs().sum(0)
+        assert bool(((r.dw.double() - dw).abs() <= lim).all()), "dw"
+
+
+@pytest.mark.parametrize("dt", list(DT))
+@pytest.mark.parametrize("n", [8191, 8192, 8193, 16385, 20000])
+def test_lists_of_tokens_longer_than_a_pass(head, tc, dt, n):
+    """8192 tokens are listed at a time; later ones follow, and their targets are looked at"""
+    v, h = 300, 32
+    x, w, t = inputs(n, v, h, dt, 25, skip=0.3)
+    weight = torch.rand(n, device="cuda") / n
+    t[-1], t[8100], t[5] = v - 1, 0, IGNORE
+    t[-3] = v + 7
+    r = head.linear_xent_step(x, w, t, weight)
+    assert tc.device_errors() == tc.TC_KERR_BAD_INDEX
+    check_large(r, x, w, t, weight, dt)
+    loss, lse = head.linear_xent(x, w, t)
+    assert tc.device_errors() == tc.TC_KERR_BAD_INDEX
+    assert torch.equal(loss, r.loss) and torch.equal(lse, r.lse)
+
+
+@pytest.mark.parametrize("dt", list(DT))
+@pytest.mark.parametrize("n,v,h,skip", [(4096, 50257, 32, 0.1), (3000, 40000, 513, 0.0)])
+def test_more_tiles_than_workgroups(head, dt, n, v, h, skip):
+    """several tiles of 256 x 256 for each workgroup, and softmax passes over several blocks of vocabulary entries"""
+    x, w, t = inputs(n, v, h, dt, 26, skip=skip)
+    weight = (torch.rand(n, device="cuda") + 0.5) / n
+    r = head.linear_xent_step(x, w, t, weight)
+    check_large(r, x, w, t, weight, dt)
+    loss, lse = head.linear_xent(x, w, t)
+    check_large(type("R", (), {"loss": loss, "lse": lse})(), x, w, t, weight, dt)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_more_than_32_tiles_for_each_workgroup(head, dt):
+    """tiles are dealt out by the die then, an eighth of them in a row for each"""
+    n, v, h = 8192, 70001, 32
+    x, w, t = inputs(n, v, h, dt, 27)
+    weight = torch.full((n,), 1.0 / n, device="cuda")
+    check_large(head.linear_xent_step(x, w, t, weight), x, w, t, weight, dt)
+    loss, lse = head.linear_xent(x, w, t)
+    check_large(type("R", (), {"loss": loss, "lse": lse})(), x, w, t, weight, dt)
+    head.free_workspaces()
