@@ -1,5 +1,6 @@
 // k_head.hip -- the loss of a model's last stage: softmax cross entropy of
-// x w^T over a large vocabulary, and its gradients, without the logits.
+// x w^T over a large vocabulary, and its gradients.  No logit is stored; with
+// gradients, softmax numerators of a chunk of tokens are.
 //
 //   z = x w^T,  lse_i = log sum_v exp z_iv,  loss_i = lse_i - z_{i,t_i}
 //   d_iv = g_i (exp(z_iv - lse_i) - [v = t_i]),  dx = d w,  dw = d^T x
@@ -82,7 +83,9 @@ template <typename V8, int J> struct Cfg;
 // 256 x 256, one workgroup of 8 wavefronts per compute unit.  For fewer tokens
 // 128 x 128 and 128 x 64, two of 4 and 2 wavefronts: those products are bound
 // by reading w, and with 256-row tiles a vocabulary of 32000 keeps half of the
-// device busy (one token, h 4096: 70 us, with 128 rows 54 us, 4.8 TB/s).
+// device busy (h 4096, w not in the caches: one token 101 us, in 128 x 128 66,
+// in 128 x 64 60, 4.4 TB/s; vocabulary of 131072 320, 231 and 213; 100 tokens
+// 101 and 65).
 template <typename V8> struct Cfg<V8, 256> : Gemm<V8, 4, 2, 2, 4, 4> { static constexpr uint32_t PER_CU = 1; };
 template <typename V8> struct Cfg<V8, 128> : Gemm<V8, 2, 2, 2, 2, 4> { static constexpr uint32_t PER_CU = 2; };
 template <typename V8> struct Cfg<V8, 64> : Gemm<V8, 2, 2, 2, 1, 6> { static constexpr uint32_t PER_CU = 2; };
@@ -390,8 +393,11 @@ __device__ __forceinline__ Tile tile_of(uint32_t t, uint32_t ni, uint32_t nj) {
 
 // The n-th of a workgroup's tiles out of `total` (false: it has no more).
 // Many tiles: every die takes an eighth of them in a row; few: every round of
-// tiles is dealt out anew (131072 x 8192 x 4096, 64 rounds: 1318 TFLOP/s
-// against 1282; 50304 x 4096 x 768, 12 rounds: 954 against 984).
+// tiles is dealt out anew.  (Losses in a row against dealt out, us, vocabularies
+// of 16384 to 131072, 4096 to 8192 tokens.  h 4096: 12 rounds 1318, 1327; 16
+// 1641, 1658; 24 2448, 2494; 32 3252, 3330; 64 6503, 6650.  h 2048: 12 693,
+// 693; 24 1282, 1290; 32 1695, 1722; 64 3354, 3450.  h 768: 12 316, 317; 16 388,
+// 383; 24 555, 557; 32 730, 722; 64 1444, 1427.)
 __device__ __forceinline__ bool nth_tile(uint32_t n, uint32_t total, uint32_t& t) {
   if (total >= 32u * gridDim.x) {
     const uint32_t per = (total + 7u) >> 3, local = n * (gridDim.x >> 3) + (blockIdx.x >> 3);
@@ -578,7 +584,7 @@ __global__ __launch_bounds__(SNT) void k_head_loss(const HeadArgs a, uint32_t c0
 }
 
 // --------------------------------- d: softmax minus target, times the weight
-// A workgroup takes 128 tokens by up to 256 vocabulary entries, a lane half a
+// A workgroup takes 128 tokens by up to 128 vocabulary entries, a lane half a
 // row of a block (32 bytes) at a time: one pass over the memory, bound by it.
 
 template <typename T, int J, bool LOW>

@@ -196,7 +196,7 @@ struct HeadArgs {
   uint32_t dw_grid, dw_parts;   // workgroups of dw's product; parts of its last round's tiles
   bool d_low;                   // d has a second plane of 16 bits (16-bit types)
   bool dw_small;                // 128 x 64 tiles, not 256 x 256
-  float* dw_part;        // [tiles of the last round][dw_parts][a tile]
+  float* dw_part;        // [dw_parts][tiles of the last round][a tile]
 };
 // bytes that the per-token buffers of a chunk may take unless the caller chooses
 constexpr uint64_t HEAD_CHUNK_BYTES = 4ull << 30;
